@@ -44,7 +44,7 @@ typedef enum {
     PQ_ERR_ALLOC = -7        /* device or host allocation failed                         */
 } pq_status;
 
-typedef enum { PQ_F16 = 0, PQ_F32 = 1 } pq_dtype;
+typedef enum { PQ_F16 = 0, PQ_F32 = 1, PQ_BF16 = 2 /* paged caches only */ } pq_dtype;
 typedef enum { PQ_CODES_K = 0, PQ_CODES_V = 1 } pq_code_kind;
 
 typedef struct {
@@ -232,6 +232,131 @@ int pq_stream_read_probe(pq_attn_ctx *ctx, const void *src /* device */, int64_t
 /* Synchronises the device, returns the sticky device error word in *flags and
  * clears it.  Bit 0: an append overflowed max_context. */
 int pq_attn_device_error(pq_attn_ctx *ctx, uint32_t *flags /* host */);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The paged 8-bit cache: keys and values of many requests in blocks that any request can hold, one byte a value and
+ * one scale for each block and KV head.  It serves what comes before and beside the PQ cache above: prompts are
+ * attended and kept in 8 bits, their tokens read back (pq_paged_read gives what pq_encode_append takes) once they
+ * are to be product-quantized.
+ *
+ * Blocks.  n_blocks blocks of block_tokens tokens.  Sequence b holds block_table[b][0 .. ceil(len / block_tokens) - 1];
+ * its token at position p is in slot block_table[b][p / block_tokens] * block_tokens + p % block_tokens.  Requests may
+ * name the same blocks (a shared prefix) as long as none of them appends to a shared one.
+ *
+ * Values.  With x the values of one KV head's tokens in a block (K and V each for itself):
+ *     scale = max(max |x|, 127 * 2^-40) / 127, rounded to fp32;  code = x / scale, rounded to the nearest integer, ties
+ *     to the even one (the exact quotient decides);  the value that the cache holds is code * scale.
+ * An append that brings a larger |x| to a block that has tokens already raises the block's scale from s to s', and the
+ * older codes c become c * s / s', rounded in the same way.  If a value is not finite, the block's scale is NaN until
+ * the block is begun anew: whoever attends over one of its tokens gets NaN.
+ *
+ * Layout.  k_cache, v_cache: pq_paged_cache_bytes() bytes each, every byte code + 128; k_scale, v_scale float32
+ * [n_blocks][Hkv].  K is [n_blocks][Hkv][block_tokens][d]; V is [n_blocks][Hkv][block_tokens / 16] pieces of 16 tokens
+ * as [d / 64][token / 4 % 4][d % 16][d / 16 % 4][token % 4], so that a lane's 16 bytes are what it multiplies.
+ *
+ * Device tensors are 16-byte aligned, token strides (in elements) multiples of 16 bytes (PQ_ERR_SHAPE otherwise).  A
+ * block number or slot outside the cache is never followed: its tokens are left out (not written, not attended over, read
+ * as nothing) and bit 1 of the device error word is set.  Lengths are clamped to [0, max_blocks * block_tokens].
+ * Calls on one context must be stream-ordered with each other, replays of graphs that recorded them included (they
+ * share the context's scratch); one context for each stream otherwise.
+ * --------------------------------------------------------------------------------------------------------------- */
+typedef struct pq_paged_ctx pq_paged_ctx;
+
+typedef struct {
+    int32_t max_seqs;     /* sequences of one call at most, 1 .. 4096                         */
+    int32_t max_tokens;   /* new tokens of one call at most, over all sequences, 1 .. 2^20    */
+    int32_t n_q_heads;    /* Hq                                                              */
+    int32_t n_kv_heads;   /* Hkv, Hq % Hkv == 0; query head h reads KV head h / (Hq / Hkv)    */
+    int32_t head_dim;     /* d; supported: 64, 128                                           */
+    int32_t block_tokens; /* supported: 16, 32, 64                                           */
+    int32_t n_blocks;     /* blocks of the cache, n_blocks * block_tokens < 2^31              */
+    int32_t max_blocks;   /* row length of the block tables, max_blocks * block_tokens <= 2^24 */
+    int32_t dtype;        /* pq_dtype of q, new and read K/V, and out                         */
+    int32_t device;       /* HIP device ordinal                                              */
+    int32_t reserved;     /* must be 0                                                       */
+} pq_paged_config;
+
+/* As pq_attn_validate_config, pq_attn_codes_bytes, pq_attn_create and pq_attn_destroy: the bytes are those of
+ * k_cache, or of v_cache. */
+int pq_paged_validate_config(const pq_paged_config *cfg /* host */);
+int64_t pq_paged_cache_bytes(const pq_paged_config *cfg /* host */);
+int pq_paged_create(const pq_paged_config *cfg /* host */, pq_paged_ctx **out /* host */);
+int pq_paged_destroy(pq_paged_ctx *ctx);
+
+/* Blocks and slots for the next step of n_seqs requests, from their lengths, all on the device.
+ *
+ *   n_new        device [n_seqs] int32    tokens that request b brings; negative: it has ended, its blocks go back
+ *   n_tokens     rows of the step's tensors: at least the sum of the n_new that are not negative
+ *   seq_len      device [n_seqs] int32    tokens cached now
+ *   free_list    device [n_blocks] int32  a stack of free blocks, the top at free_count - 1; changed in place
+ *   free_count   device [1] int32         blocks on it
+ *   block_table  device [n_seqs][max_blocks] int32; new blocks are written behind those that a request has
+ *   new_seq_len, new_free_count           lengths and count after the step (may be the same arrays as seq_len, free_count)
+ *   tok_start    device [n_seqs + 1] int32  row of request b's first new token: the requests' tokens lie one after another
+ *   tok_len      device [n_seqs] int32    new tokens that have a place: n_new, or 0
+ *   slot_map     device [n_tokens] int32  slot of each new token; -1 where it has none
+ *
+ * First the ended requests' blocks are pushed, in the order of the requests and of their tables, and their lengths become 0.
+ * Then the requests take the blocks they need from the top, in order.  A request gets all its tokens or none: none if
+ * it would be longer than max_blocks * block_tokens, if its rows end behind n_tokens, or if it needs blocks and there are not
+ * enough for it and all that have asked before it (those that got none for this reason included); it keeps its length
+ * then, and bit 0 of the device error word is set.
+ * 1 <= n_seqs <= max_seqs, 0 <= n_tokens <= max_tokens, else PQ_ERR_CAPACITY (PQ_ERR_SHAPE if below). */
+int pq_paged_plan(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const int32_t *n_new, const int32_t *seq_len,
+                  int32_t *free_list, const int32_t *free_count, int32_t *block_table, int32_t *new_seq_len,
+                  int32_t *new_free_count, int32_t *tok_start, int32_t *tok_len, int32_t *slot_map, void *hip_stream);
+
+/* Quantizes n_tokens rows of keys and values into their slots.
+ *
+ *   new_k/new_v  device, row t at t * kv_stride elements, [Hkv][d] dtype there (kv_stride >= Hkv * d)
+ *   slot_map     device [n_tokens] int32; a row with a negative slot is passed over
+ *
+ * The slots of one block are those of rows in a row, ascending by one, as pq_paged_plan gives them (a block that is written
+ * from two places of the map, or a slot that comes twice, leaves that block's contents unspecified, no other's).  Tokens of
+ * the block in front of the first such slot are older ones and are kept; a block whose slot 0 is written begins anew.
+ * 0 <= n_tokens <= max_tokens; 0 does nothing. */
+int pq_paged_append(pq_paged_ctx *ctx, int32_t n_tokens, const void *new_k, const void *new_v, int64_t kv_stride,
+                    const int32_t *slot_map, uint8_t *k_cache, uint8_t *v_cache, float *k_scale, float *v_scale,
+                    void *hip_stream);
+
+/* Tokens of the cache in full precision: row r of sequence b is its token first[b] + r.
+ *
+ *   n_rows       rows per sequence, >= 0
+ *   first        device [n_seqs] int32, >= 0; NULL: all 0
+ *   out_k/out_v  device [n_seqs][Hkv][n_rows][d] dtype, what pq_encode_append takes; rows behind a sequence's last
+ *                token are left as they were */
+int pq_paged_read(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_rows, const uint8_t *k_cache, const uint8_t *v_cache,
+                  const float *k_scale, const float *v_scale, const int32_t *block_table, const int32_t *seq_len,
+                  const int32_t *first, void *out_k, void *out_v, void *hip_stream);
+
+/* Attention of one query token per sequence over all its seq_len[b] tokens (its own, appended before, among them):
+ * out = sum_t softmax_t(scale * q . k_t) v_t.
+ *
+ *   q            device, row b at b * q_stride elements, [Hq][d] dtype there (q_stride >= Hq * d)
+ *   scale        as in pq_attn_decode
+ *   out          device [n_seqs][Hq][d] dtype; a sequence without tokens gets a row of zeros */
+int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_stride, const uint8_t *k_cache,
+                    const uint8_t *v_cache, const float *k_scale, const float *v_scale, const int32_t *block_table,
+                    const int32_t *seq_len, float scale, void *out, void *hip_stream);
+
+/* Causal attention of the tokens that a step has brought (appended before): rows tok_start[b] .. tok_start[b] +
+ * tok_len[b] - 1 of q are the last tok_len[b] tokens of sequence b, and row i of them attends over the first
+ * seq_len[b] - tok_len[b] + i + 1 tokens (a row for which that is not positive gets zeros).
+ *
+ *   n_tokens             rows of q and out, >= the end of the last sequence's rows
+ *   q                    as in pq_paged_decode, row t at t * q_stride elements
+ *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
+ *   tok_start, tok_len   device int32, as pq_paged_plan gives them; rows outside [0, n_tokens) are left out
+ *   out                  device [n_tokens][Hq][d] dtype; rows of no sequence are left as they were
+ *
+ * 0 <= n_tokens <= max_tokens; 0 does nothing. */
+int pq_paged_prefill(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const void *q, int64_t q_stride,
+                     const uint8_t *k_cache, const uint8_t *v_cache, const float *k_scale, const float *v_scale,
+                     const int32_t *block_table, const int32_t *seq_len, const int32_t *tok_start, const int32_t *tok_len,
+                     float scale, void *out, void *hip_stream);
+
+/* As pq_attn_device_error.  Bit 0: pq_paged_plan refused a request; bit 1: a block number or slot outside the cache. */
+int pq_paged_device_error(pq_paged_ctx *ctx, uint32_t *flags /* host */);
 
 /* Static, never NULL. */
 const char *pq_status_string(int status);

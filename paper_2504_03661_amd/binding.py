@@ -15,7 +15,7 @@ import os
 from dataclasses import dataclass
 from typing import Optional
 
-PQ_F16, PQ_F32 = 0, 1
+PQ_F16, PQ_F32, PQ_BF16 = 0, 1, 2       # PQ_BF16: paged caches only
 PQ_CODES_K, PQ_CODES_V = 0, 1
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -55,6 +55,30 @@ class PQAttnConfig:
 
     def c_struct(self) -> _Config:
         return _Config(*(int(getattr(self, n)) for n, _ in _Config._fields_))
+
+
+class _PagedConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "max_seqs", "max_tokens", "n_q_heads", "n_kv_heads", "head_dim", "block_tokens", "n_blocks", "max_blocks", "dtype",
+        "device", "reserved")]
+
+
+@dataclass
+class PQPagedConfig:
+    max_seqs: int
+    max_tokens: int
+    n_q_heads: int
+    n_kv_heads: int
+    n_blocks: int
+    max_blocks: int
+    head_dim: int = 128
+    block_tokens: int = 16
+    dtype: int = PQ_F16
+    device: int = 0
+    reserved: int = 0
+
+    def c_struct(self) -> _PagedConfig:
+        return _PagedConfig(*(int(getattr(self, n)) for n, _ in _PagedConfig._fields_))
 
 
 def library_path() -> str:
@@ -111,6 +135,27 @@ def load_library():
     L.pq_stream_read_probe.argtypes = [vp, vp, ctypes.c_int64, vp]
     L.pq_attn_device_error.restype = ctypes.c_int
     L.pq_attn_device_error.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
+    pagedp = ctypes.POINTER(_PagedConfig)
+    L.pq_paged_validate_config.restype = ctypes.c_int
+    L.pq_paged_validate_config.argtypes = [pagedp]
+    L.pq_paged_cache_bytes.restype = i64
+    L.pq_paged_cache_bytes.argtypes = [pagedp]
+    L.pq_paged_create.restype = ctypes.c_int
+    L.pq_paged_create.argtypes = [pagedp, ctypes.POINTER(vp)]
+    L.pq_paged_destroy.restype = ctypes.c_int
+    L.pq_paged_destroy.argtypes = [vp]
+    L.pq_paged_plan.restype = ctypes.c_int
+    L.pq_paged_plan.argtypes = [vp, i32, i32] + [vp] * 11
+    L.pq_paged_append.restype = ctypes.c_int
+    L.pq_paged_append.argtypes = [vp, i32, vp, vp, i64] + [vp] * 6
+    L.pq_paged_read.restype = ctypes.c_int
+    L.pq_paged_read.argtypes = [vp, i32, i32] + [vp] * 10
+    L.pq_paged_decode.restype = ctypes.c_int
+    L.pq_paged_decode.argtypes = [vp, i32, vp, i64] + [vp] * 6 + [f32, vp, vp]
+    L.pq_paged_prefill.restype = ctypes.c_int
+    L.pq_paged_prefill.argtypes = [vp, i32, i32, vp, i64] + [vp] * 8 + [f32, vp, vp]
+    L.pq_paged_device_error.restype = ctypes.c_int
+    L.pq_paged_device_error.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
     L.pq_status_string.restype = ctypes.c_char_p
     L.pq_status_string.argtypes = [ctypes.c_int]
     _calls = calls
@@ -264,3 +309,92 @@ def pq_attn_device_error(ctx) -> int:
     flags = ctypes.c_uint32(0)
     _check(load_library().pq_attn_device_error(ctx, ctypes.byref(flags)), "pq_attn_device_error")
     return int(flags.value)
+
+
+def pq_paged_validate_config(cfg: PQPagedConfig) -> int:
+    return int(load_library().pq_paged_validate_config(ctypes.byref(cfg.c_struct())))
+
+
+def pq_paged_cache_bytes(cfg: PQPagedConfig) -> int:
+    n = int(load_library().pq_paged_cache_bytes(ctypes.byref(cfg.c_struct())))
+    if n < 0:
+        raise PQAttnError(n, "pq_paged_cache_bytes")
+    return n
+
+
+def pq_paged_create(cfg: PQPagedConfig) -> int:
+    out = ctypes.c_void_p()
+    _check(load_library().pq_paged_create(ctypes.byref(cfg.c_struct()), ctypes.byref(out)), "pq_paged_create")
+    return out.value
+
+
+def pq_paged_destroy(ctx: int) -> None:
+    _check(load_library().pq_paged_destroy(ctx), "pq_paged_destroy")
+
+
+def pq_paged_plan(ctx, n_seqs, n_tokens, n_new, seq_len, free_list, free_count, block_table, new_seq_len, new_free_count,
+                  tok_start, tok_len, slot_map, stream=None) -> None:
+    _check(load_library().pq_paged_plan(ctx, int(n_seqs), int(n_tokens), _addr(n_new), _addr(seq_len), _addr(free_list),
+                                        _addr(free_count), _addr(block_table), _addr(new_seq_len), _addr(new_free_count),
+                                        _addr(tok_start), _addr(tok_len), _addr(slot_map), _stream(stream)), "pq_paged_plan")
+
+
+def pq_paged_append(ctx, n_tokens, new_k, new_v, kv_stride, slot_map, k_cache, v_cache, k_scale, v_scale, stream=None) -> None:
+    _check(load_library().pq_paged_append(ctx, int(n_tokens), _addr(new_k), _addr(new_v), int(kv_stride), _addr(slot_map),
+                                          _addr(k_cache), _addr(v_cache), _addr(k_scale), _addr(v_scale), _stream(stream)),
+           "pq_paged_append")
+
+
+def pq_paged_read(ctx, n_seqs, n_rows, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, first, out_k, out_v,
+                  stream=None) -> None:
+    _check(load_library().pq_paged_read(ctx, int(n_seqs), int(n_rows), _addr(k_cache), _addr(v_cache), _addr(k_scale),
+                                        _addr(v_scale), _addr(block_table), _addr(seq_len), _addr(first), _addr(out_k),
+                                        _addr(out_v), _stream(stream)), "pq_paged_read")
+
+
+def pq_paged_decode(ctx, n_seqs, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, scale, out,
+                    stream=None) -> None:
+    _check(load_library().pq_paged_decode(ctx, int(n_seqs), _addr(q), int(q_stride), _addr(k_cache), _addr(v_cache),
+                                          _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len), float(scale),
+                                          _addr(out), _stream(stream)), "pq_paged_decode")
+
+
+def pq_paged_prefill(ctx, n_seqs, n_tokens, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, tok_start,
+                     tok_len, scale, out, stream=None) -> None:
+    _check(load_library().pq_paged_prefill(ctx, int(n_seqs), int(n_tokens), _addr(q), int(q_stride), _addr(k_cache),
+                                           _addr(v_cache), _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len),
+                                           _addr(tok_start), _addr(tok_len), float(scale), _addr(out), _stream(stream)),
+           "pq_paged_prefill")
+
+
+def pq_paged_device_error(ctx) -> int:
+    flags = ctypes.c_uint32(0)
+    _check(load_library().pq_paged_device_error(ctx, ctypes.byref(flags)), "pq_paged_device_error")
+    return int(flags.value)
+
+
+class PQPaged:
+    """A context of pq_paged_create, destroyed with the object; `handle` is what the pq_paged_* calls take."""
+
+    handle: Optional[int] = None
+
+    def __init__(self, cfg: PQPagedConfig):
+        self.cfg = cfg
+        self.handle = pq_paged_create(cfg)
+
+    def close(self) -> None:
+        if self.handle is not None:
+            handle, self.handle = self.handle, None
+            pq_paged_destroy(handle)
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:       # at the interpreter's end the library may be gone
+            pass

@@ -55,22 +55,6 @@ int noalloc_lookup(int dev, noalloc_device *out)
     return PQ_OK;
 }
 
-struct device_guard {
-    int prev = -1;
-    bool ok = false;
-    explicit device_guard(int dev)
-    {
-        if (hipGetDevice(&prev) != hipSuccess)
-            return;
-        ok = (prev == dev) || (hipSetDevice(dev) == hipSuccess);
-    }
-    ~device_guard()
-    {
-        if (ok && prev >= 0)
-            (void)hipSetDevice(prev);
-    }
-};
-
 int validate(const pq_attn_config *c)
 {
     if (c == nullptr)

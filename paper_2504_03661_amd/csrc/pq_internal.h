@@ -185,6 +185,23 @@ struct pq_encode_args {
     const uint64_t *grid_state;  // pq_attn_ctx::grid_state
 };
 
+// makes a device current and puts the one before back
+struct device_guard {
+    int prev = -1;
+    bool ok = false;
+    explicit device_guard(int dev)
+    {
+        if (hipGetDevice(&prev) != hipSuccess)
+            return;
+        ok = (prev == dev) || (hipSetDevice(dev) == hipSuccess);
+    }
+    ~device_guard()
+    {
+        if (ok && prev >= 0)
+            (void)hipSetDevice(prev);
+    }
+};
+
 // launchers (each returns hipGetLastError() after its launches)
 hipError_t pq_launch_decode(const pq_attn_ctx *ctx, const pq_decode_args &a, hipStream_t s);
 hipError_t pq_launch_decode_grouped(const pq_attn_ctx *ctx, const pq_decode_args &a, hipStream_t s);
