@@ -13,10 +13,19 @@
 #define PQ_PAGED_ERRFLAG_REFUSED 1u
 #define PQ_PAGED_ERRFLAG_RANGE 2u
 
+// how pq_paged_decode's workgroups are cut out, and what they exchange through
+struct pq_paged_decode_plan {
+    float *partials;        // [head group][2 budget slots][sub_rows][d + 2]: maximum, sum, sums of values
+    unsigned int *tickets;  // one per slot, zero between calls
+    int n_sub, sub_rows;    // head groups of a KV head, and query heads of one (the last may have fewer)
+    int budget;             // chunks per head group that a call's tokens are cut into
+};
+
 struct pq_paged_ctx {
     pq_paged_config cfg;
     int log_block;          // log2(block_tokens)
     int n_cu;
+    pq_paged_decode_plan decode;
     int *plan;              // scratch of pq_paged_plan: PQ_PAGED_PLAN_ARRAYS arrays of max_seqs + 1
     unsigned int *dev_err;  // sticky error word
 };
@@ -81,6 +90,10 @@ struct pq_paged_attn_args {
 hipError_t pq_launch_paged_plan(const pq_paged_ctx *ctx, const pq_paged_plan_args &a, hipStream_t s);
 hipError_t pq_launch_paged_append(const pq_paged_ctx *ctx, const pq_paged_append_args &a, hipStream_t s);
 hipError_t pq_launch_paged_read(const pq_paged_ctx *ctx, const pq_paged_read_args &a, hipStream_t s);
+pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu);
+int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
+int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
+hipError_t pq_launch_paged_decode(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 hipError_t pq_launch_paged_attn(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 
 // Byte of token r (of its block) and dim d in the V bytes of one block and head: pieces of 16 tokens, in each

@@ -72,6 +72,8 @@ pq_paged_view view(const pq_paged_ctx *ctx, const uint8_t *k, const uint8_t *v, 
 
 void free_ctx(pq_paged_ctx *ctx)
 {
+    if (ctx->decode.partials) (void)hipFree(ctx->decode.partials);
+    if (ctx->decode.tickets) (void)hipFree(ctx->decode.tickets);
     if (ctx->plan) (void)hipFree(ctx->plan);
     if (ctx->dev_err) (void)hipFree(ctx->dev_err);
     delete ctx;
@@ -99,7 +101,9 @@ int attend(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const void *q, i
     a.n_tokens = n_tokens;
     a.Hq = ctx->cfg.n_q_heads;
     a.G = ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads;
-    return pq_launch_paged_attn(ctx, a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
+    const hipError_t e = tok_start == nullptr ? pq_launch_paged_decode(ctx, a, (hipStream_t)hip_stream)
+                                              : pq_launch_paged_attn(ctx, a, (hipStream_t)hip_stream);
+    return e == hipSuccess ? PQ_OK : PQ_ERR_HIP;
 }
 
 }  // namespace
@@ -141,7 +145,12 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     ctx->log_block = cfg->block_tokens == 16 ? 4 : cfg->block_tokens == 32 ? 5 : 6;
     ctx->n_cu = n_cu;
     const size_t plan_bytes = (size_t)PQ_PAGED_PLAN_ARRAYS * (cfg->max_seqs + 1) * sizeof(int);
+    ctx->decode = pq_paged_plan_decode(cfg, n_cu);
+    const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
+    const size_t part_bytes = (size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float);
     bool ok = hipMalloc((void **)&ctx->plan, plan_bytes) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->decode.partials, part_bytes) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->decode.tickets, slots * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->dev_err, sizeof(unsigned int)) == hipSuccess;
     if (!ok) {
         (void)hipGetLastError();
@@ -149,6 +158,8 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
         return PQ_ERR_ALLOC;
     }
     ok = hipMemset(ctx->plan, 0, plan_bytes) == hipSuccess;
+    ok = ok && hipMemset(ctx->decode.partials, 0, part_bytes) == hipSuccess;
+    ok = ok && hipMemset(ctx->decode.tickets, 0, slots * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMemset(ctx->dev_err, 0, sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipDeviceSynchronize() == hipSuccess;
     if (!ok) {

@@ -1,0 +1,412 @@
+// pq_paged_decode: one query token per sequence over the paged 8-bit cache.
+//
+// A workgroup has one sequence, the up to 16 query heads of one KV head (more go to further workgroups) and a chunk of the
+// sequence's tokens; its four wavefronts share the chunk out.  Scores are S^T = K Q^T, 16 tokens by 16 query heads per matrix
+// instruction: in the result a lane holds four tokens of one head, which is what the second product, O^T = V^T W, takes as its
+// right operand — weights go from one to the other in registers, and a head's maximum, sum and rescaling are its lanes' own.
+// The dims of K and the tokens of V may come in any order as long as both operands of a product agree: K's rows are read 16
+// bytes a lane as they lie in memory, V is stored so that a lane's 16 bytes are four dims' worth of its four tokens.
+// No byte passes through LDS before the end.
+//
+// Chunks: all of a call's chunks are about equally long, so long sequences are cut into many and the chip is evenly filled
+// whatever the lengths are.  Every workgroup works the cut out for itself from the lengths.  A sequence of several
+// chunks is put together by the workgroup that finishes last (pq_device_utils.h, exchange of split partials).
+//
+// Bound by HBM: 2 d bytes per token and KV head.
+#include <hip/hip_runtime.h>
+
+#include "pq_paged_tile.h"
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = 16;
+constexpr int STEP = 32;                // tokens a wavefront takes at a time
+constexpr int CHUNK_ALIGN = WAVES * STEP;
+
+// What a lane keeps of 64 blocks in a row of a sequence
+struct block_batch {
+    int first;  // number of the first one in the sequence
+    int id;     // 0 where there is none
+    float k_scale, v_log, v_inv;
+};
+
+__device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane)
+{
+    block_batch x;
+    x.first = first;
+    const int j = first + lane;
+    int id = j < last ? table[j] : -1;
+    const bool there = (unsigned)id < (unsigned)c.n_blocks;
+    if (j < last && !there)
+        paged_error(c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+    x.id = there ? id : 0;
+    x.k_scale = 0.0f;  // no such block: every score is -inf, every weight 0
+    x.v_log = -INFINITY;
+    x.v_inv = 0.0f;
+    if (there) {
+        const int64_t at = (int64_t)id * c.Hkv + h;
+        const float v = value_scale(c.v_scale[at]);
+        x.k_scale = c.k_scale[at];
+        x.v_log = __log2f(v);
+        x.v_inv = 1.0f / v;
+    }
+    return x;
+}
+
+__device__ inline float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+
+// Two pieces of 16 tokens as they lie in memory, and their blocks' scales
+template <int D> struct step_data {
+    u32x4 k[2][D / 64], v[2][D / 64];
+    float k_scale[2], v_log[2], v_inv[2];
+};
+
+template <int D>
+__device__ inline void load_step(const pq_paged_view &c, const int32_t *table, block_batch &batch, int last_block, int h, int t,
+                                 int lane, step_data<D> &s)
+{
+    const int k_at = (lane & 15) * D + (lane >> 4) * 16, v_at = lane * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = t + 16 * i, j = p >> c.log_block;
+        if (j >= batch.first + 64)
+            batch = load_batch(c, table, j, last_block, h, lane);
+        const int at = j - batch.first;
+        const int id = __builtin_amdgcn_readlane(batch.id, at);
+        s.k_scale[i] = lane_of(batch.k_scale, at);
+        s.v_log[i] = lane_of(batch.v_log, at);
+        s.v_inv[i] = lane_of(batch.v_inv, at);
+        const int64_t base = (((int64_t)id * c.Hkv + h) << c.log_block) * D + (p & ((1 << c.log_block) - 1)) * D;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+            s.k[i][x] = __builtin_nontemporal_load((const u32x4 *)(c.k + base + k_at + 64 * x));
+            s.v[i][x] = __builtin_nontemporal_load((const u32x4 *)(c.v + base + v_at + 1024 * x));
+        }
+    }
+}
+
+// sum over the wavefront's lanes before this one and itself
+__device__ inline int64_t lane_scan(int64_t x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(x, d, 64);
+        if (lane >= d)
+            x += y;
+    }
+    return x;
+}
+
+struct chunk_place {
+    int b, len;        // sequence and its length; b < 0: no chunk for this workgroup
+    int first, chunks; // the sequence's first chunk in the numbering, and how many it has
+    int slot;          // of its first chunk among the chunks of sequences that have several
+    int tokens;        // of a chunk
+};
+
+__device__ inline int chunk_tokens(int64_t total, int budget)
+{
+    const int64_t share = (total + budget - 1) / budget;
+    const int n = share < PQ_MAX_TOKENS ? (int)share : PQ_MAX_TOKENS;
+    return n > 0 ? (n + CHUNK_ALIGN - 1) / CHUNK_ALIGN * CHUNK_ALIGN : CHUNK_ALIGN;
+}
+
+// Chunk number c of a call.  Sequence after sequence is cut into pieces of the same length, total / budget rounded up: that
+// makes at most budget + n_seqs - 1 chunks (an empty sequence has one, somebody writes its zeros), and those of sequences
+// with several are at most 2 budget.
+__device__ inline chunk_place find_chunk(const pq_paged_attn_args &a, int budget, int c, int lane)
+{
+    chunk_place p;
+    p.b = -1;
+    if (a.n_seqs == 1) {
+        p.len = paged_length(a.c, 0);
+        p.tokens = chunk_tokens(p.len, budget);
+        p.chunks = p.len > 0 ? (p.len + p.tokens - 1) / p.tokens : 1;
+        p.first = p.slot = 0;
+        if (c < p.chunks)
+            p.b = 0;
+        return p;
+    }
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64)
+        total += b0 + lane < a.n_seqs ? paged_length(a.c, b0 + lane) : 0;
+    p.tokens = chunk_tokens(__shfl(lane_scan(total, lane), 63, 64), budget);
+    int before = 0, slots = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
+        int len = 0, n = 0;
+        if (b0 + lane < a.n_seqs) {
+            len = paged_length(a.c, b0 + lane);
+            n = len > 0 ? (len + p.tokens - 1) / p.tokens : 1;
+        }
+        // both running sums at once: chunks, and (above) chunks of sequences that have several
+        const int64_t sums = lane_scan(n + ((int64_t)(n > 1 ? n : 0) << 32), lane);
+        const int upto = before + (int)(sums & 0xffffffff), slot = slots + (int)(sums >> 32) - (n > 1 ? n : 0);
+        const uint64_t mine = __ballot(c >= upto - n && c < upto);
+        if (mine != 0) {
+            const int l = __builtin_ctzll(mine);
+            p.b = b0 + l;
+            p.len = __builtin_amdgcn_readlane(len, l);
+            p.chunks = __builtin_amdgcn_readlane(n, l);
+            p.first = __builtin_amdgcn_readlane(upto - n, l);
+            p.slot = __builtin_amdgcn_readlane(slot, l);
+            break;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+        slots += __builtin_amdgcn_readlane((int)(sums >> 32), 63);
+    }
+    return p;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_attn_args a, pq_paged_decode_plan w)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;  // two fp16 parts of queries and weights
+    constexpr int PARTS = SPLIT ? 2 : 1;
+    constexpr int DT = D / 16;
+    __shared__ float part[WAVES][ROWS][D + 4];
+    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS], row_m[ROWS], row_l[ROWS];
+    __shared__ int last_one;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int n_groups = a.c.Hkv * w.n_sub, group = blockIdx.x % n_groups, chunk = blockIdx.x / n_groups;
+    const chunk_place p = find_chunk(a, w.budget, chunk, lane);
+    if (p.b < 0)
+        return;
+    const int h = group / w.n_sub, sub = group - h * w.n_sub;
+    const int head0 = h * a.G + sub * w.sub_rows;
+    const int rows = a.G - sub * w.sub_rows < w.sub_rows ? a.G - sub * w.sub_rows : w.sub_rows;
+    const int col = lane & 15, quad = lane >> 4;
+
+    // this wavefront's tokens
+    const int from = (chunk - p.first) * p.tokens, upto = from + p.tokens < p.len ? from + p.tokens : p.len;
+    const int share = ((upto - from + WAVES - 1) / WAVES + STEP - 1) / STEP * STEP;
+    const int t0 = from + wave * share, t1 = t0 + share < upto ? t0 + share : upto;
+    const int32_t *table = a.c.table + (int64_t)p.b * a.c.max_blocks;
+    const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block;
+
+    step_data<D> now, next;
+    block_batch batch;
+    if (t0 < t1) {
+        batch = load_batch(a.c, table, t0 >> a.c.log_block, last_block, h, lane);
+        load_step<D>(a.c, table, batch, last_block, h, t0, lane, now);
+    }
+
+    // queries: lane has row `col`, dims 64 x + 16 quad + 0 .. 15, as the instruction's k index takes K's bytes
+    half8v q[PARTS][D / 32];
+    float per_score;  // what a dot product of codes is multiplied by, but for the block's scale
+    {
+        float x[D / 4];
+        const T *src = (const T *)a.q + (int64_t)p.b * a.q_stride + (int64_t)(head0 + (col < rows ? col : 0)) * D + quad * 16;
+        float high = 0.0f;
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            paged_load8(src + 64 * i, x + 16 * i);
+            paged_load8(src + 64 * i + 8, x + 16 * i + 8);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 4; ++i)
+            high = fmaxf(high, fabsf(x[i]));
+        high = fmaxf(high, __shfl_xor(high, 16, 64));
+        high = fmaxf(high, __shfl_xor(high, 32, 64));
+        const int e = query_exponent(high);
+        per_score = ldexpf(a.scale_log2e, -e);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float v = ldexpf(x[8 * s + j], e);
+                q[0][s][j] = (_Float16)v;
+                if (SPLIT)
+                    q[PARTS - 1][s][j] = (_Float16)(v - (float)q[0][s][j]);
+            }
+    }
+
+    f32x4 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+        o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    float m = LOWEST, l = 0.0f;
+    for (int t = t0; t < t1; t += STEP) {
+        const bool more = t + STEP < t1;
+        if (more)
+            load_step<D>(a.c, table, batch, last_block, h, t + STEP, lane, next);
+        float s[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f32x4 dot = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < D / 32; ++x) {
+                const half8v k = codes8(now.k[i][x >> 1][2 * (x & 1)], now.k[i][x >> 1][2 * (x & 1) + 1]);
+#pragma unroll
+                for (int part_ = 0; part_ < PARTS; ++part_)
+                    dot = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[part_][x], dot, 0, 0, 0);
+            }
+            const float by = per_score * now.k_scale[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s[4 * i + j] = fmaf(dot[j], by, now.v_log[i]);
+        }
+        if (t + STEP > t1)  // the last step: tokens behind the end
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (t + 16 * (i >> 2) + 4 * quad + (i & 3) >= t1)
+                    s[i] = -INFINITY;
+        float high = s[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i)
+            high = fmaxf(high, s[i]);
+        if (__ballot(high > m + MAX_SLACK) != 0) {
+            high = fmaxf(high, __shfl_xor(high, 16, 64));
+            high = fmaxf(high, __shfl_xor(high, 32, 64));
+            const float moved = fmaxf(m, high), down = __builtin_amdgcn_exp2f(m - moved);
+            m = moved;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+                o[i] *= down;
+        }
+        const float base = m - WEIGHT_BITS;
+        half8v weights[PARTS];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = __builtin_amdgcn_exp2f(s[4 * i + j] - base);
+                sum += x;
+                weights[0][4 * i + j] = (_Float16)x;
+                if (SPLIT)
+                    weights[PARTS - 1][4 * i + j] = (_Float16)(x - (float)weights[0][4 * i + j]);
+            }
+            l = fmaf(sum, now.v_inv[i], l);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i) {
+            const half8v v = codes8(now.v[0][i >> 2][i & 3], now.v[1][i >> 2][i & 3]);
+#pragma unroll
+            for (int part_ = 0; part_ < PARTS; ++part_)
+                o[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, weights[part_], o[i], 0, 0, 0);
+        }
+        if (more)
+            now = next;
+    }
+
+    // the wavefronts' parts of the chunk
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    if (quad == 0) {
+        wave_m[wave][col] = m;
+        wave_l[wave][col] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+        *(f32x4 *)&part[wave][col][16 * i + 4 * quad] = o[i];
+    __syncthreads();
+    if (threadIdx.x < ROWS) {
+        const int r = threadIdx.x;
+        float top = wave_m[0][r], sum = 0.0f;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i)
+            top = fmaxf(top, wave_m[i][r]);
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float down = __builtin_amdgcn_exp2f(wave_m[i][r] - top);
+            sum = fmaf(wave_l[i][r], down, sum);
+            wave_m[i][r] = down;
+        }
+        row_m[r] = top;
+        row_l[r] = sum;
+    }
+    __syncthreads();
+    T *const out = (T *)a.out + ((int64_t)p.b * a.Hq + head0) * D;
+    const int64_t slot0 = (int64_t)group * (2 * w.budget) + p.slot;
+    float *const parts = w.partials + slot0 * w.sub_rows * (D + 2);  // of the sequence's first chunk
+    const int per_chunk = w.sub_rows * (D + 2);
+    float *const mine = parts + (int64_t)(chunk - p.first) * per_chunk;
+    for (int i = threadIdx.x; i < rows * (D / 2); i += THREADS) {
+        const int r = i / (D / 2), d = i % (D / 2) * 2;
+        float x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            x = fmaf(part[k][r][d], wave_m[k][r], x);
+            y = fmaf(part[k][r][d + 1], wave_m[k][r], y);
+        }
+        if (p.chunks == 1) {
+            const float sum = row_l[r], by = sum == 0.0f ? 0.0f : 1.0f / sum;
+            out[r * D + d] = paged_elem<T>::down(x * by);
+            out[r * D + d + 1] = paged_elem<T>::down(y * by);
+        } else {
+            publish(mine + r * (D + 2) + 2 + d, x, y);
+        }
+    }
+    if (p.chunks == 1)
+        return;
+    if (threadIdx.x < rows)
+        publish(mine + threadIdx.x * (D + 2), row_m[threadIdx.x], row_l[threadIdx.x]);
+    publish_wait();
+    __syncthreads();
+    unsigned int *ticket = w.tickets + slot0;
+    if (threadIdx.x == 0)
+        last_one = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)(p.chunks - 1);
+    __syncthreads();
+    if (!last_one)
+        return;
+    if (threadIdx.x == 0)
+        ticket_reset(ticket);
+    for (int i = threadIdx.x; i < rows * (D / 2); i += THREADS) {
+        const int r = i / (D / 2), d = i % (D / 2) * 2;
+        float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll 4
+        for (int c = 0; c < p.chunks; ++c) {
+            const float2 ml = fetch(parts + (int64_t)c * per_chunk + r * (D + 2));
+            const float2 v = fetch(parts + (int64_t)c * per_chunk + r * (D + 2) + 2 + d);
+            const float high = fmaxf(top, ml.x), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
+            top = high;
+            sum = fmaf(ml.y, by, sum * old);
+            x = fmaf(v.x, by, x * old);
+            y = fmaf(v.y, by, y * old);
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        out[r * D + d] = paged_elem<T>::down(x * by);
+        out[r * D + d + 1] = paged_elem<T>::down(y * by);
+    }
+}
+
+}  // namespace
+
+// Chunks are as many as keep the chip busy (PER_CU workgroups a compute unit), not more than a merge reads in a few
+// microseconds.
+pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu)
+{
+    constexpr int PER_CU = 2, MOST = 128;
+    pq_paged_decode_plan w;
+    const int G = cfg->n_q_heads / cfg->n_kv_heads;
+    w.n_sub = (G + ROWS - 1) / ROWS;
+    w.sub_rows = (G + w.n_sub - 1) / w.n_sub;
+    w.n_sub = (G + w.sub_rows - 1) / w.sub_rows;
+    const int groups = cfg->n_kv_heads * w.n_sub, wanted = PER_CU * n_cu / groups;
+    w.budget = wanted < 1 ? 1 : wanted > MOST ? MOST : wanted;
+    w.partials = nullptr;
+    w.tickets = nullptr;
+    return w;
+}
+
+int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_plan &w)
+{
+    return (int64_t)cfg->n_kv_heads * w.n_sub * 2 * w.budget;
+}
+
+int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w)
+{
+    return (int64_t)w.sub_rows * (cfg->head_dim + 2);
+}
+
+hipError_t pq_launch_paged_decode(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s)
+{
+    const pq_paged_decode_plan &w = ctx->decode;
+    const unsigned grid = (unsigned)(a.c.Hkv * w.n_sub) * (unsigned)(w.budget + a.n_seqs - 1);
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_decode_kernel<T, D>), dim3(grid), dim3(THREADS), 0, s, a, w)
+    PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);
+#undef LAUNCH
+    return hipGetLastError();
+}

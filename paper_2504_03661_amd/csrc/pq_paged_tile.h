@@ -1,0 +1,52 @@
+// Pieces that the two attention kernels over the paged 8-bit cache share (gfx950).
+//
+// Both form scores and values with fp16 matrix instructions.  A code is an integer of at most 7 bits and sign: exact in fp16.  A
+// query row is multiplied by a power of two that brings its largest element to [2^13, 2^14) and rounded to fp16: what is 11 or
+// fewer bits wide (fp16, bf16) stays exact down to 2^-27 of the row's largest element; fp32 rows are split into two fp16
+// parts, 22 bits.  Products and sums are fp32.  A block's key scale multiplies the finished dot product; its value scale goes into
+// the weights' exponent:
+//     s_t = log2(e) scale q.k_t + log2(v_scale_t),   w_t = 2^(s_t - m + 13),   out = sum_t w_t code_t / sum_t w_t / v_scale_t
+// with m near the largest s_t, so that the weights — rounded to fp16 (fp32 contexts: to two parts) — keep 11 bits down to 2^-27 of
+// the largest and never leave fp16's range.
+#pragma once
+
+#include "pq_device_utils.h"
+#include "pq_paged.h"
+
+namespace {
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef _Float16 half4v __attribute__((ext_vector_type(4)));
+typedef _Float16 half8v __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr float WEIGHT_BITS = 13.0f;  // log2 of the largest weight, before m's slack
+constexpr float LOWEST = -3.0e38f;     // m of a row that has seen nothing
+constexpr float MAX_SLACK = 2.0f;     // m is moved when a score is more than this above it: weights stay below 2^15
+
+// Four bytes (code + 128) as fp16 codes: 0x6400 | byte is 1024 + byte, and 1152 less is the code.
+__device__ inline half4v codes4(uint32_t w)
+{
+    const half2v bias = {(_Float16)1152.0f, (_Float16)1152.0f};
+    const half2v lo = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, w, 0x04010400u)) - bias;
+    const half2v hi = __builtin_bit_cast(half2v, __builtin_amdgcn_perm(0x64646464u, w, 0x04030402u)) - bias;
+    return half4v{lo.x, lo.y, hi.x, hi.y};
+}
+
+__device__ inline half8v codes8(uint32_t w0, uint32_t w1)
+{
+    const half4v a = codes4(w0), b = codes4(w1);
+    return half8v{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+}
+
+// A block's value scale: never below 2^-40, which a block that nothing was written to would be (a NaN stays).
+__device__ inline float value_scale(float v) { return v < 0x1p-40f ? 0x1p-40f : v; }
+
+// the exponent by which a row of queries is scaled, from its largest |element|
+__device__ inline int query_exponent(float largest)
+{
+    const int e = (int)(__float_as_uint(largest) >> 23);  // 0: no row element above the subnormal numbers
+    return e == 0 ? 0 : 13 + 127 - e;
+}
+
+}  // namespace
