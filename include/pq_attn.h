@@ -346,7 +346,8 @@ int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_
  *   n_tokens             rows of q and out, >= the end of the last sequence's rows
  *   q                    as in pq_paged_decode, row t at t * q_stride elements
  *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
- *   tok_start, tok_len   device int32, as pq_paged_plan gives them; rows outside [0, n_tokens) are left out
+ *   tok_start, tok_len   device int32, as pq_paged_plan gives them (rows from n_tokens on are left out, a sequence whose
+ *                        first row is outside [0, n_tokens) altogether)
  *   out                  device [n_tokens][Hq][d] dtype; rows of no sequence are left as they were
  *
  * 0 <= n_tokens <= max_tokens; 0 does nothing. */

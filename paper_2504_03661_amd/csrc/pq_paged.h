@@ -21,11 +21,20 @@ struct pq_paged_decode_plan {
     int budget;             // chunks per head group that a call's tokens are cut into
 };
 
+// the same of pq_paged_prefill
+struct pq_paged_prefill_plan {
+    float *partials;        // [KV head][slots][rows of a tile][d + 2]
+    unsigned int *tickets;  // one per slot, zero between calls
+    int budget;             // pieces per KV head that a call with few tiles is cut into
+    int slots;              // pieces that there can be then
+};
+
 struct pq_paged_ctx {
     pq_paged_config cfg;
     int log_block;          // log2(block_tokens)
     int n_cu;
     pq_paged_decode_plan decode;
+    pq_paged_prefill_plan prefill;
     int *plan;              // scratch of pq_paged_plan: PQ_PAGED_PLAN_ARRAYS arrays of max_seqs + 1
     unsigned int *dev_err;  // sticky error word
 };
@@ -94,7 +103,9 @@ pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu);
 int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
 int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
 hipError_t pq_launch_paged_decode(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
-hipError_t pq_launch_paged_attn(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
+pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu);
+int64_t pq_paged_prefill_slot_floats(const pq_paged_config *cfg);
+hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 
 // Byte of token r (of its block) and dim d in the V bytes of one block and head: pieces of 16 tokens, in each
 // [d / 64][r / 4][d % 16][d / 16 % 4][r % 4].  The 16 bytes that share all but the last two are four dims' worth of four tokens:

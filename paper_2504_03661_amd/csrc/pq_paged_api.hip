@@ -74,6 +74,8 @@ void free_ctx(pq_paged_ctx *ctx)
 {
     if (ctx->decode.partials) (void)hipFree(ctx->decode.partials);
     if (ctx->decode.tickets) (void)hipFree(ctx->decode.tickets);
+    if (ctx->prefill.partials) (void)hipFree(ctx->prefill.partials);
+    if (ctx->prefill.tickets) (void)hipFree(ctx->prefill.tickets);
     if (ctx->plan) (void)hipFree(ctx->plan);
     if (ctx->dev_err) (void)hipFree(ctx->dev_err);
     delete ctx;
@@ -102,7 +104,7 @@ int attend(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const void *q, i
     a.Hq = ctx->cfg.n_q_heads;
     a.G = ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads;
     const hipError_t e = tok_start == nullptr ? pq_launch_paged_decode(ctx, a, (hipStream_t)hip_stream)
-                                              : pq_launch_paged_attn(ctx, a, (hipStream_t)hip_stream);
+                                              : pq_launch_paged_prefill(ctx, a, (hipStream_t)hip_stream);
     return e == hipSuccess ? PQ_OK : PQ_ERR_HIP;
 }
 
@@ -148,7 +150,12 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     ctx->decode = pq_paged_plan_decode(cfg, n_cu);
     const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
     const size_t part_bytes = (size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float);
+    ctx->prefill = pq_paged_plan_prefill(cfg, n_cu);
+    const int64_t tiles = (int64_t)cfg->n_kv_heads * ctx->prefill.slots;
+    const size_t tile_bytes = (size_t)tiles * pq_paged_prefill_slot_floats(cfg) * sizeof(float);
     bool ok = hipMalloc((void **)&ctx->plan, plan_bytes) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->prefill.partials, tile_bytes) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->prefill.tickets, tiles * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->decode.partials, part_bytes) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->decode.tickets, slots * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->dev_err, sizeof(unsigned int)) == hipSuccess;
@@ -158,8 +165,8 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
         return PQ_ERR_ALLOC;
     }
     ok = hipMemset(ctx->plan, 0, plan_bytes) == hipSuccess;
-    ok = ok && hipMemset(ctx->decode.partials, 0, part_bytes) == hipSuccess;
     ok = ok && hipMemset(ctx->decode.tickets, 0, slots * sizeof(unsigned int)) == hipSuccess;
+    ok = ok && hipMemset(ctx->prefill.tickets, 0, tiles * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMemset(ctx->dev_err, 0, sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipDeviceSynchronize() == hipSuccess;
     if (!ok) {

@@ -23,38 +23,6 @@ constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = 16;
 constexpr int STEP = 32;                // tokens a wavefront takes at a time
 constexpr int CHUNK_ALIGN = WAVES * STEP;
 
-// What a lane keeps of 64 blocks in a row of a sequence
-struct block_batch {
-    int first;  // number of the first one in the sequence
-    int id;     // 0 where there is none
-    float k_scale, v_log, v_inv;
-};
-
-__device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane)
-{
-    block_batch x;
-    x.first = first;
-    const int j = first + lane;
-    int id = j < last ? table[j] : -1;
-    const bool there = (unsigned)id < (unsigned)c.n_blocks;
-    if (j < last && !there)
-        paged_error(c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
-    x.id = there ? id : 0;
-    x.k_scale = 0.0f;  // no such block: every score is -inf, every weight 0
-    x.v_log = -INFINITY;
-    x.v_inv = 0.0f;
-    if (there) {
-        const int64_t at = (int64_t)id * c.Hkv + h;
-        const float v = value_scale(c.v_scale[at]);
-        x.k_scale = c.k_scale[at];
-        x.v_log = __log2f(v);
-        x.v_inv = 1.0f / v;
-    }
-    return x;
-}
-
-__device__ inline float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
-
 // Two pieces of 16 tokens as they lie in memory, and their blocks' scales
 template <int D> struct step_data {
     u32x4 k[2][D / 64], v[2][D / 64];
@@ -83,18 +51,6 @@ __device__ inline void load_step(const pq_paged_view &c, const int32_t *table, b
             s.v[i][x] = __builtin_nontemporal_load((const u32x4 *)(c.v + base + v_at + 1024 * x));
         }
     }
-}
-
-// sum over the wavefront's lanes before this one and itself
-__device__ inline int64_t lane_scan(int64_t x, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d, 64);
-        if (lane >= d)
-            x += y;
-    }
-    return x;
 }
 
 struct chunk_place {

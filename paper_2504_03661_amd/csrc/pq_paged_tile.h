@@ -10,6 +10,8 @@
 // the largest and never leave fp16's range.
 #pragma once
 
+#include <cfloat>
+
 #include "pq_device_utils.h"
 #include "pq_paged.h"
 
@@ -47,6 +49,50 @@ __device__ inline int query_exponent(float largest)
 {
     const int e = (int)(__float_as_uint(largest) >> 23);  // 0: no row element above the subnormal numbers
     return e == 0 ? 0 : 13 + 127 - e;
+}
+
+// What a lane keeps of 64 blocks in a row of a sequence
+struct block_batch {
+    int first;  // number of the first one in the sequence
+    int id;     // 0 where there is none
+    float k_scale, v_log, v_inv;
+};
+
+__device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane)
+{
+    block_batch x;
+    x.first = first;
+    const int j = first + lane;
+    int id = j < last ? table[j] : -1;
+    const bool there = (unsigned)id < (unsigned)c.n_blocks;
+    if (j < last && !there)
+        paged_error(c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+    x.id = there ? id : 0;
+    x.k_scale = 0.0f;  // no such block: every score is -inf, every weight 0
+    x.v_log = -INFINITY;
+    x.v_inv = 0.0f;
+    if (there) {
+        const int64_t at = (int64_t)id * c.Hkv + h;
+        const float v = value_scale(c.v_scale[at]);
+        x.k_scale = c.k_scale[at];
+        x.v_log = __log2f(v);
+        x.v_inv = v <= FLT_MAX ? 1.0f / v : 0.0f;  // (a NaN is in v_log: a row that does not see the block adds 0 times this)
+    }
+    return x;
+}
+
+__device__ inline float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
+
+// sum over the wavefront's lanes before this one and itself
+__device__ inline int64_t lane_scan(int64_t x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t y = __shfl_up(x, d, 64);
+        if (lane >= d)
+            x += y;
+    }
+    return x;
 }
 
 }  // namespace

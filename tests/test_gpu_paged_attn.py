@@ -140,6 +140,10 @@ def test_not_finite_blocks_reach_their_readers_only():
     pq.pq_paged_prefill(ctx.handle, 1, 100, q, q.shape[1], *c.args(), dev([0, 100]), dev([100]),
                         0.09, out)
     assert not out[:32].isnan().any() and out[32:, :2].isnan().all() and not out[:, 2:].isnan().any()
+    args = list(c.args())
+    args[4], args[5] = args[4][1:], args[5][1:]
+    pq.pq_paged_prefill(ctx.handle, 1, 100, q, q.shape[1], *args, dev([0, 100]), dev([100]), 0.09, out)
+    assert not out[:96].isnan().any() and out[96:, 2:].isnan().all() and not out[:, :2].isnan().any()
 
 
 def test_blocks_outside_the_cache_are_left_out():
