@@ -13,8 +13,8 @@ CALLS_SOURCE = os.path.join(CSRC, "pq_binding.cpp")
 CALLS = os.path.join(HERE, "_pq_calls" + sysconfig.get_config_var("EXT_SUFFIX"))    # for this interpreter
 SOURCES = ["pq12_codes.hip", "pq12_decode.hip", "pq12_decode_grouped.hip", "pq_api.hip", "pq_decode.hip", "pq_decode_grouped.hip", "pq_encode.hip", "pq_kmeans.hip", "pq_layout.hip",
            "pq_paged_api.hip", "pq_paged_cache.hip",
-           "pq_paged_decode.hip", "pq_paged_plan.hip", "pq_paged_prefill.hip"]
-HEADERS = [os.path.join(CSRC, "pq_internal.h"), os.path.join(CSRC, "pq_device_utils.h"), os.path.join(CSRC, "pq_nearest_filter.h"), os.path.join(CSRC, "pq_nearest_grid.h"), os.path.join(CSRC, "pq_filter_constants.h"), os.path.join(CSRC, "pq_paged.h"), os.path.join(CSRC, "pq_paged_tile.h"),
+           "pq_paged_decode.hip", "pq_paged_few.hip", "pq_paged_plan.hip", "pq_paged_prefill.hip"]
+HEADERS = [os.path.join(CSRC, "pq_internal.h"), os.path.join(CSRC, "pq_device_utils.h"), os.path.join(CSRC, "pq_nearest_filter.h"), os.path.join(CSRC, "pq_nearest_grid.h"), os.path.join(CSRC, "pq_filter_constants.h"), os.path.join(CSRC, "pq_paged.h"), os.path.join(CSRC, "pq_paged_tile.h"), os.path.join(CSRC, "pq_paged_work.h"),
            os.path.join(ROOT, "include", "pq_attn.h")]
 
 # packed-fp32 instructions are switched off for all device code; -ffp-contract=off keeps

@@ -21,12 +21,15 @@ struct pq_paged_decode_plan {
     int budget;             // chunks per head group that a call's tokens are cut into
 };
 
-// the same of pq_paged_prefill
+// How pq_paged_prefill shares out a call: sequences of at most few_rows rows (tokens times query heads of a KV head) in tiles of
+// PQ_PAGED_FEW_ROWS, the others in tiles of PQ_PAGED_TILE_ROWS.  Budgets: pieces per KV head that a call of few tiles is cut
+// into along the keys; 0: not cut.  Partials: [KV head][slots][rows of a tile][d + 2], maximum, sum, sums of values.
+#define PQ_PAGED_TILE_ROWS 256
+#define PQ_PAGED_FEW_ROWS 32
 struct pq_paged_prefill_plan {
-    float *partials;        // [KV head][slots][rows of a tile][d + 2]
-    unsigned int *tickets;  // one per slot, zero between calls
-    int budget;             // pieces per KV head that a call with few tiles is cut into
-    int slots;              // pieces that there can be then
+    float *tile_partials, *few_partials;
+    int tile_budget, tile_slots, few_budget, few_slots;
+    int few_rows;
 };
 
 struct pq_paged_ctx {
@@ -104,7 +107,8 @@ int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_
 int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
 hipError_t pq_launch_paged_decode(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu);
-int64_t pq_paged_prefill_slot_floats(const pq_paged_config *cfg);
+int64_t pq_paged_prefill_partials(const pq_paged_config *cfg, const pq_paged_prefill_plan &w, bool few);  // floats
+hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int dtype, int dim, int64_t entries, hipStream_t s);
 hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 
 // Byte of token r (of its block) and dim d in the V bytes of one block and head: pieces of 16 tokens, in each
@@ -167,12 +171,12 @@ __device__ inline void paged_error(unsigned int *word, unsigned int flag) { atom
 #define PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH)                                                              \
     do {                                                                                                  \
         if ((dim) == 128) {                                                                               \
-            if ((dtype) == PQ_F16) LAUNCH(__half, 128);                                                   \
-            else if ((dtype) == PQ_BF16) LAUNCH(__hip_bfloat16, 128);                                     \
-            else LAUNCH(float, 128);                                                                      \
+            if ((dtype) == PQ_F16) { LAUNCH(__half, 128); }                                               \
+            else if ((dtype) == PQ_BF16) { LAUNCH(__hip_bfloat16, 128); }                                 \
+            else { LAUNCH(float, 128); }                                                                  \
         } else {                                                                                          \
-            if ((dtype) == PQ_F16) LAUNCH(__half, 64);                                                    \
-            else if ((dtype) == PQ_BF16) LAUNCH(__hip_bfloat16, 64);                                      \
-            else LAUNCH(float, 64);                                                                       \
+            if ((dtype) == PQ_F16) { LAUNCH(__half, 64); }                                                \
+            else if ((dtype) == PQ_BF16) { LAUNCH(__hip_bfloat16, 64); }                                  \
+            else { LAUNCH(float, 64); }                                                                   \
         }                                                                                                 \
     } while (0)

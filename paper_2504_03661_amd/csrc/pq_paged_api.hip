@@ -74,8 +74,8 @@ void free_ctx(pq_paged_ctx *ctx)
 {
     if (ctx->decode.partials) (void)hipFree(ctx->decode.partials);
     if (ctx->decode.tickets) (void)hipFree(ctx->decode.tickets);
-    if (ctx->prefill.partials) (void)hipFree(ctx->prefill.partials);
-    if (ctx->prefill.tickets) (void)hipFree(ctx->prefill.tickets);
+    if (ctx->prefill.tile_partials) (void)hipFree(ctx->prefill.tile_partials);
+    if (ctx->prefill.few_partials) (void)hipFree(ctx->prefill.few_partials);
     if (ctx->plan) (void)hipFree(ctx->plan);
     if (ctx->dev_err) (void)hipFree(ctx->dev_err);
     delete ctx;
@@ -151,11 +151,11 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
     const size_t part_bytes = (size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float);
     ctx->prefill = pq_paged_plan_prefill(cfg, n_cu);
-    const int64_t tiles = (int64_t)cfg->n_kv_heads * ctx->prefill.slots;
-    const size_t tile_bytes = (size_t)tiles * pq_paged_prefill_slot_floats(cfg) * sizeof(float);
+    const size_t tile_bytes = (size_t)pq_paged_prefill_partials(cfg, ctx->prefill, false) * sizeof(float);
+    const size_t few_bytes = (size_t)pq_paged_prefill_partials(cfg, ctx->prefill, true) * sizeof(float);
     bool ok = hipMalloc((void **)&ctx->plan, plan_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->prefill.partials, tile_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->prefill.tickets, tiles * sizeof(unsigned int)) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->prefill.tile_partials, tile_bytes) == hipSuccess;
+    ok = ok && hipMalloc((void **)&ctx->prefill.few_partials, few_bytes) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->decode.partials, part_bytes) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->decode.tickets, slots * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMalloc((void **)&ctx->dev_err, sizeof(unsigned int)) == hipSuccess;
@@ -166,7 +166,6 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     }
     ok = hipMemset(ctx->plan, 0, plan_bytes) == hipSuccess;
     ok = ok && hipMemset(ctx->decode.tickets, 0, slots * sizeof(unsigned int)) == hipSuccess;
-    ok = ok && hipMemset(ctx->prefill.tickets, 0, tiles * sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipMemset(ctx->dev_err, 0, sizeof(unsigned int)) == hipSuccess;
     ok = ok && hipDeviceSynchronize() == hipSuccess;
     if (!ok) {

@@ -1,0 +1,368 @@
+// pq_paged_prefill's other kernel, for sequences that bring few tokens: chunks, guessed tokens, the odd step among prompts.
+// And what both of them share: the merge of pieces, and the launches.
+//
+// A workgroup has 32 rows (a token's query heads of a KV head side by side) and a piece of the keys that they see, of which each
+// of its four wavefronts takes a part, as pq_paged_decode's do: bytes go from memory to the lanes that multiply them, with
+// no LDS between.  The products are those of the kernel for many rows, 32x32x16, with K's dims in the order that 16-byte loads
+// bring them and V's dims in that of its 16-byte words.
+//
+// Bound by HBM where a sequence has one or two tiles, then by the conversion of bytes, which every tile does for itself.
+#include <hip/hip_runtime.h>
+
+#include "pq_paged_work.h"
+
+namespace {
+
+constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = PQ_PAGED_FEW_ROWS, STEP = 32;
+
+// 32 keys as they lie in memory, and their blocks' scales
+template <int D> struct step_bytes {
+    u32x4 k[D / 32];
+    uint32_t v[2][2][D / 32];  // [piece of 16 tokens][token quad half, half + 2][product]
+    float k_scale[2], v_log[2], v_inv[2];
+};
+
+template <int D>
+__device__ inline void load_bytes(const pq_paged_view &c, const int32_t *table, block_batch &batch, int last_block, int h, int t, int lane,
+                                  step_bytes<D> &s)
+{
+    const int col = lane & 31, half = lane >> 5;
+    int64_t base[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int p = t + 16 * i, j = p >> c.log_block;
+        if (j >= batch.first + 64)
+            batch = load_batch(c, table, j, last_block, h, lane);
+        const int at = j - batch.first;
+        const int id = __builtin_amdgcn_readlane(batch.id, at);
+        s.k_scale[i] = lane_of(batch.k_scale, at);
+        s.v_log[i] = lane_of(batch.v_log, at);
+        s.v_inv[i] = lane_of(batch.v_inv, at);
+        base[i] = (((int64_t)id * c.Hkv + h) << c.log_block) * D + (p & ((1 << c.log_block) - 1)) * D;
+    }
+    const uint8_t *k = c.k + (col < 16 ? base[0] : base[1]) + (col & 15) * D + 16 * half;
+#pragma unroll
+    for (int x = 0; x < D / 32; ++x)
+        s.k[x] = *(const u32x4 *)(k + 32 * x);
+    // 128 dims: a lane's row is dim 64 (col / 16) + 16 k + col % 16 in product k, the four of a 16-byte word; 64 dims: 32 (col / 16)
+    // + 16 k + col % 16, half a word
+    const int v_at = (D == 128 ? (col >> 4) * 1024 : (col >> 4) * 8) + (col & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const uint8_t *v = c.v + base[i] + v_at + (half + 2 * q) * 256;
+            if constexpr (D == 128) {
+                const u32x4 w = *(const u32x4 *)v;
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+                    s.v[i][q][x] = w[x];
+            } else {
+                const u32x2 w = *(const u32x2 *)v;
+                s.v[i][q][0] = w[0];
+                s.v[i][q][1] = w[1];
+            }
+        }
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_kernel(pq_paged_attn_args a, pq_paged_prefill_plan w)
+{
+    constexpr bool SPLIT = sizeof(T) == 4;  // two fp16 parts of queries and weights
+    constexpr int PARTS = SPLIT ? 2 : 1, DT = D / 32;
+    __shared__ float part[WAVES][ROWS][D + 4];
+    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS], row_m[ROWS], row_l[ROWS];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int h = blockIdx.x % a.c.Hkv, entry = blockIdx.x / a.c.Hkv;
+    work_place p;
+    if (!find_work(a, work_rule{1, w.few_rows, ROWS, w.few_budget}, entry, lane, p))
+        return;
+    const tile_place tile(p, a.G, ROWS);
+    if (p.split >= tile.pieces)
+        return;
+    const int k0 = p.split * p.keys, k1 = k0 + p.keys < tile.sees ? k0 + p.keys : tile.sees;
+    const int share = ((k1 - k0 + WAVES - 1) / WAVES + STEP - 1) / STEP * STEP;
+    const int t0 = k0 + wave * share, t1 = t0 + share < k1 ? t0 + share : k1;
+    const int32_t *table = a.c.table + (int64_t)p.b * a.c.max_blocks;
+    const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block;
+    step_bytes<D> now, next;
+    block_batch batch;
+    if (t0 < t1) {
+        batch = load_batch(a.c, table, t0 >> a.c.log_block, last_block, h, lane);
+        load_bytes<D>(a.c, table, batch, last_block, h, t0, lane, now);
+    }
+
+    const int col = lane & 31, half = lane >> 5;
+    const bool there = col < tile.rows;
+    const int token = there ? (tile.row0 + col) / a.G : 0, head = there ? tile.row0 + col - token * a.G : 0;
+    int sees = there ? p.past + token + 1 : 0;
+    sees = sees < t1 ? sees : t1;
+    const int least = __builtin_amdgcn_readfirstlane(tile.rows == ROWS ? p.past + tile.row0 / a.G + 1 : 0);  // (of the first row)
+    half8v q[PARTS][D / 16];
+    float per_score;
+    {
+        // dims 32 x + 16 half + 0 .. 15 of the row, as K's loads bring them
+        float v[D / 2];
+        float high = 0.0f;
+        const T *src = (const T *)a.q + (int64_t)(p.first_row + token) * a.q_stride + (int64_t)(h * a.G + head) * D + 16 * half;
+#pragma unroll
+        for (int x = 0; x < D / 32; ++x) {
+            paged_load8(src + 32 * x, v + 16 * x);
+            paged_load8(src + 32 * x + 8, v + 16 * x + 8);
+        }
+#pragma unroll
+        for (int i = 0; i < D / 2; ++i)
+            high = fmaxf(high, fabsf(v[i]));
+        high = fmaxf(high, __shfl_xor(high, 32, 64));
+        const int e = query_exponent(high);
+        per_score = ldexpf(a.scale_log2e, -e);
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = ldexpf(v[8 * x + j], e);
+                q[0][x][j] = (_Float16)f;
+                if (SPLIT)
+                    q[PARTS - 1][x][j] = (_Float16)(f - (float)q[0][x][j]);
+            }
+    }
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            o[i][j] = 0.0f;
+    float m = LOWEST, l = 0.0f;
+    for (int t = t0; t < t1; t += STEP) {
+        const bool more = t + STEP < t1;
+        if (more)
+            load_bytes<D>(a.c, table, batch, last_block, h, t + STEP, lane, next);
+        f32x16 dot;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            dot[j] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+            const half8v k = codes8(now.k[x >> 1][2 * (x & 1)], now.k[x >> 1][2 * (x & 1) + 1]);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+                dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][x], dot, 0, 0, 0);
+        }
+        float s[16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float by = per_score * now.k_scale[i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s[8 * i + j] = fmaf(dot[8 * i + j], by, now.v_log[i]);
+        }
+        if (t + STEP > least || t + STEP > t1)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (t + 8 * (j >> 2) + 4 * half + (j & 3) >= sees)
+                    s[j] = -INFINITY;
+        float high = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j)
+            high = fmaxf(high, s[j]);
+        if (__ballot(high > m + MAX_SLACK) != 0) {
+            high = fmaxf(high, __shfl_xor(high, 32, 64));
+            const float moved = fmaxf(m, high), down = __builtin_amdgcn_exp2f(m - moved);
+            m = moved;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    o[i][j] *= down;
+        }
+        const float base = m - WEIGHT_BITS;
+        half8v weights[PARTS][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = __builtin_amdgcn_exp2f(s[8 * i + j] - base);
+                sum += x;
+                weights[0][i][j] = (_Float16)x;
+                if (SPLIT)
+                    weights[PARTS - 1][i][j] = (_Float16)(x - (float)weights[0][i][j]);
+            }
+            l = fmaf(sum, now.v_inv[i], l);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const half8v v = codes8(now.v[x][0][i], now.v[x][1][i]);
+#pragma unroll
+                for (int j = 0; j < PARTS; ++j)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[j][x], o[i], 0, 0, 0);
+            }
+        if (more)
+            now = next;
+    }
+
+    // the wavefronts' parts
+    l += __shfl_xor(l, 32, 64);
+    if (half == 0) {
+        wave_m[wave][col] = m;
+        wave_l[wave][col] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < DT; ++i)
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {
+            const int d = (D == 128 ? 64 * (j >> 3) + 16 * i : 32 * (j >> 3) + 16 * i) + 8 * ((j >> 2) & 1) + 4 * half;
+            *(f32x4 *)&part[wave][col][d] = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+        }
+    __syncthreads();
+    if (threadIdx.x < ROWS) {
+        const int r = threadIdx.x;
+        float top = wave_m[0][r], sum = 0.0f;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i)
+            top = fmaxf(top, wave_m[i][r]);
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float down = __builtin_amdgcn_exp2f(wave_m[i][r] - top);
+            sum = fmaf(wave_l[i][r], down, sum);
+            wave_m[i][r] = down;
+        }
+        row_m[r] = top;
+        row_l[r] = sum;
+    }
+    __syncthreads();
+    float *const to = w.few_partials + ((int64_t)h * w.few_slots + p.slot + p.split) * (ROWS * (D + 2));
+    for (int i = threadIdx.x; i < tile.rows * (D / 2); i += THREADS) {
+        const int r = i / (D / 2), d = i % (D / 2) * 2;
+        float x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < WAVES; ++k) {
+            x = fmaf(part[k][r][d], wave_m[k][r], x);
+            y = fmaf(part[k][r][d + 1], wave_m[k][r], y);
+        }
+        if (tile.pieces == 1) {
+            const float by = row_l[r] == 0.0f ? 0.0f : 1.0f / row_l[r];
+            const int row = tile.row0 + r, t = row / a.G;
+            T *out = (T *)a.out + ((int64_t)(p.first_row + t) * a.Hq + h * a.G + (row - t * a.G)) * D + d;
+            out[0] = paged_elem<T>::down(x * by);
+            out[1] = paged_elem<T>::down(y * by);
+        } else {
+            *(float2 *)(to + r * (D + 2) + 2 + d) = make_float2(x, y);
+            if (d == 0)
+                *(float2 *)(to + r * (D + 2)) = make_float2(row_m[r], row_l[r]);
+        }
+    }
+}
+
+constexpr int MERGE_ROWS = 4;
+
+// Puts the pieces of a row's keys together: a wavefront a row (a query head of a token), two dims a lane.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * MERGE_ROWS) void pq_paged_merge_kernel(pq_paged_attn_args a, pq_paged_prefill_plan w)
+{
+    const int lane = threadIdx.x & 63;
+    const int row = blockIdx.x * MERGE_ROWS + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int token = row / a.Hq, head = row - token * a.Hq, h = head / a.G, g = head - h * a.G;
+    work_place p;
+    if (token >= a.n_tokens)
+        return;
+    const bool few = w.few_budget > 0 && find_row(a, work_rule{1, w.few_rows, ROWS, w.few_budget}, token, g, lane, p);
+    if (!few && (w.tile_budget == 0 ||
+                 !find_row(a, work_rule{w.few_rows + 1, INT32_MAX, PQ_PAGED_TILE_ROWS, w.tile_budget}, token, g, lane, p)))
+        return;
+    const tile_place tile(p, a.G, few ? ROWS : PQ_PAGED_TILE_ROWS);
+    if (tile.pieces == 1)
+        return;
+    const int64_t stride = (few ? ROWS : PQ_PAGED_TILE_ROWS) * (D + 2);
+    const int d = 2 * (lane % (D / 2)), r = (token - p.first_row) * a.G + g - tile.row0;
+    const float *from = (few ? w.few_partials + ((int64_t)h * w.few_slots + p.slot) * stride : w.tile_partials + ((int64_t)h * w.tile_slots + p.slot) * stride) + r * (D + 2);
+    float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
+    constexpr int AT_ONCE = 16;  // loads on their way together
+    for (int c0 = 0; c0 < tile.pieces; c0 += AT_ONCE, from += AT_ONCE * stride) {
+        float2 ml[AT_ONCE], v[AT_ONCE];
+#pragma unroll
+        for (int c = 0; c < AT_ONCE; ++c) {
+            const float *piece = from + (c0 + c < tile.pieces ? c : 0) * stride;
+            ml[c] = *(const float2 *)piece;
+            v[c] = *(const float2 *)(piece + 2 + d);
+        }
+#pragma unroll
+        for (int c = 0; c < AT_ONCE; ++c) {
+            const float m = c0 + c < tile.pieces ? ml[c].x : -INFINITY;  // (a repeated one counts for nothing)
+            const float high = fmaxf(top, m), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(m - high);
+            top = high;
+            sum = fmaf(ml[c].y, by, sum * old);
+            x = fmaf(v[c].x, by, x * old);
+            y = fmaf(v[c].y, by, y * old);
+        }
+    }
+    if (lane < D / 2) {
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        T *out = (T *)a.out + (int64_t)row * D + d;
+        out[0] = paged_elem<T>::down(x * by);
+        out[1] = paged_elem<T>::down(y * by);
+    }
+}
+
+}  // namespace
+
+// Pieces are as many as give every compute unit a workgroup of the kernel for many rows, or two of the one for few.
+pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu)
+{
+    pq_paged_prefill_plan w;
+    w.tile_budget = n_cu / cfg->n_kv_heads > 1 ? n_cu / cfg->n_kv_heads : 1;
+    w.few_budget = 2 * w.tile_budget;
+    w.tile_slots = 2 * w.tile_budget;
+    w.few_slots = 2 * w.few_budget;
+    w.tile_partials = w.few_partials = nullptr;
+#ifndef FEW_LIMIT
+#define FEW_LIMIT 128
+#endif
+    w.few_rows = FEW_LIMIT;
+    return w;
+}
+
+int64_t pq_paged_prefill_partials(const pq_paged_config *cfg, const pq_paged_prefill_plan &w, bool few)
+{
+    return (int64_t)cfg->n_kv_heads * (few ? w.few_slots * PQ_PAGED_FEW_ROWS : w.tile_slots * PQ_PAGED_TILE_ROWS) * (cfg->head_dim + 2);
+}
+
+hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s)
+{
+    pq_paged_prefill_plan w = ctx->prefill;
+    const int64_t rows = (int64_t)a.n_tokens * a.G, seqs = a.n_seqs < a.n_tokens ? a.n_seqs : a.n_tokens;
+    // which kernels can have work: a single sequence is taken to have all rows
+    const bool many = rows > w.few_rows;
+    if (many && a.n_seqs == 1)
+        w.few_rows = 0;
+    const int dtype = ctx->cfg.dtype, dim = ctx->cfg.head_dim;
+    // tiles there can be: every sequence's last may be a part of one.  A call that can have as many as the budget is not cut
+    // along the keys.
+    const int64_t few_tiles = rows / ROWS + seqs, tiles = rows / PQ_PAGED_TILE_ROWS + seqs;
+    if (few_tiles >= w.few_budget || w.few_rows == 0)
+        w.few_budget = 0;
+    if (tiles >= w.tile_budget || !many)
+        w.tile_budget = 0;
+    if (w.few_rows > 0) {
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.few_budget) * a.c.Hkv)), dim3(THREADS), 0, s, a, w)
+        PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
+#undef LAUNCH
+    }
+    if (many) {
+        const hipError_t e = pq_launch_paged_tiles(a, w, dtype, dim, tiles + w.tile_budget, s);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (w.few_budget > 0 || w.tile_budget > 0) {
+        const unsigned grid = (unsigned)(((int64_t)a.n_tokens * a.Hq + MERGE_ROWS - 1) / MERGE_ROWS);
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_merge_kernel<T, D>), dim3(grid), dim3(64 * MERGE_ROWS), 0, s, a, w)
+        PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
+#undef LAUNCH
+    }
+    return hipGetLastError();
+}
