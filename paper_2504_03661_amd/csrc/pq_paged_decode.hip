@@ -60,13 +60,6 @@ struct chunk_place {
     int tokens;        // of a chunk
 };
 
-__device__ inline int chunk_tokens(int64_t total, int budget)
-{
-    const int64_t share = (total + budget - 1) / budget;
-    const int n = share < PQ_MAX_TOKENS ? (int)share : PQ_MAX_TOKENS;
-    return n > 0 ? (n + CHUNK_ALIGN - 1) / CHUNK_ALIGN * CHUNK_ALIGN : CHUNK_ALIGN;
-}
-
 // Chunk number c of a call.  Sequence after sequence is cut into pieces of the same length, total / budget rounded up: that
 // makes at most budget + n_seqs - 1 chunks (an empty sequence has one, somebody writes its zeros), and those of sequences
 // with several are at most 2 budget.
@@ -76,17 +69,17 @@ __device__ inline chunk_place find_chunk(const pq_paged_attn_args &a, int budget
     p.b = -1;
     if (a.n_seqs == 1) {
         p.len = paged_length(a.c, 0);
-        p.tokens = chunk_tokens(p.len, budget);
+        p.tokens = piece_tokens((float)p.len, budget, CHUNK_ALIGN, CHUNK_ALIGN);
         p.chunks = p.len > 0 ? (p.len + p.tokens - 1) / p.tokens : 1;
         p.first = p.slot = 0;
         if (c < p.chunks)
             p.b = 0;
         return p;
     }
-    int64_t total = 0;
+    float total = 0.0f;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64)
-        total += b0 + lane < a.n_seqs ? paged_length(a.c, b0 + lane) : 0;
-    p.tokens = chunk_tokens(__shfl(lane_scan(total, lane), 63, 64), budget);
+        total += b0 + lane < a.n_seqs ? (float)paged_length(a.c, b0 + lane) : 0.0f;
+    p.tokens = piece_tokens(wave_sum(total), budget, CHUNK_ALIGN, CHUNK_ALIGN);
     int before = 0, slots = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
         int len = 0, n = 0;
@@ -94,9 +87,7 @@ __device__ inline chunk_place find_chunk(const pq_paged_attn_args &a, int budget
             len = paged_length(a.c, b0 + lane);
             n = len > 0 ? (len + p.tokens - 1) / p.tokens : 1;
         }
-        // both running sums at once: chunks, and (above) chunks of sequences that have several
-        const int64_t sums = lane_scan(n + ((int64_t)(n > 1 ? n : 0) << 32), lane);
-        const int upto = before + (int)(sums & 0xffffffff), slot = slots + (int)(sums >> 32) - (n > 1 ? n : 0);
+        const int several = n > 1 ? n : 0, upto = before + lane_scan(n), slot = slots + lane_scan(several) - several;
         const uint64_t mine = __ballot(c >= upto - n && c < upto);
         if (mine != 0) {
             const int l = __builtin_ctzll(mine);
@@ -108,7 +99,7 @@ __device__ inline chunk_place find_chunk(const pq_paged_attn_args &a, int budget
             break;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
-        slots += __builtin_amdgcn_readlane((int)(sums >> 32), 63);
+        slots = __builtin_amdgcn_readlane(slot + several, 63);
     }
     return p;
 }

@@ -231,7 +231,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv, entry = blockIdx.x / a.c.Hkv;
     work_place p;
-    if (!find_work(a, work_rule{w.few_rows + 1, INT32_MAX, TILE_ROWS, w.tile_budget}, entry, lane, p))
+    if (!find_work(a, tile_rule(w), entry, lane, p))
         return;
     const int col = lane & 31, half = lane >> 5;
     const tile_place tile(p, a.G, TILE_ROWS);
@@ -319,10 +319,16 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
         __syncthreads();
         dots_32<S, PARTS>(rows, lds[0], 0, col, half, dot);
     }
-    const int part_end = __builtin_amdgcn_readfirstlane(wave_least < k1 ? wave_least : k1);
+    // (in a vector register, and so is the branch on it: as a uniform one the compiler moves so much across it that the kernel
+    // takes 256 registers and spills 40 of them, 8K prompt 930 us instead of 597)
+    int part_end = wave_least < k1 ? wave_least : k1;
+    asm volatile("" : "+v"(part_end));
+    int last = k1;
+    asm volatile("" : "+v"(last));
     int at = 0, before = 0;  // the tile's place in LDS, and that of the tile in front of it
-    bool pending = false;    // weights whose values are still to be added
-    for (int t = k0; t < k1; t += KEYS) {
+    // one step behind the last that the wavefront's rows see: it adds that one's values, and its own weights are all 0
+    const int wave_end = wave_sees > k0 ? k0 + (wave_sees - k0 + 31) / 32 * 32 + 32 : k0;
+    for (int t = k0; t < last; t += KEYS) {
         const int next = at == BUFFERS - 1 ? 0 : at + 1;
 #pragma unroll
         for (int u = 0; u < PARTS_32; ++u) {
@@ -335,21 +341,15 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
                     load(t + 2 * KEYS);
                 __syncthreads();
             }
-            if (part + 32 <= part_end) {
+            if (part + 32 <= part_end)
                 step_32<S, PARTS, false>(rows, of_next, next_u, of_before, before_u, lds[at], u, part, col, half, dot, weights);
-                pending = true;
-            } else if (part < wave_sees) {
+            else if (part < wave_end)
                 step_32<S, PARTS, true>(rows, of_next, next_u, of_before, before_u, lds[at], u, part, col, half, dot, weights);
-                pending = true;
-            } else if (pending) {  // (before their place in LDS is another tile's)
-                values_32<S, PARTS>(rows, of_before, before_u, col, half, weights);
-                pending = false;
-            }
         }
         before = at;
         at = next;
     }
-    if (pending)
+    if (k0 < k1)
         values_32<S, PARTS>(rows, lds[before], PARTS_32 - 1, col, half, weights);
 
     float *const part = w.tile_partials + ((int64_t)h * w.tile_slots + p.slot + p.split) * (TILE_ROWS * (D + 2));

@@ -83,16 +83,30 @@ __device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *
 
 __device__ inline float lane_of(float x, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane)); }
 
-// sum over the wavefront's lanes before this one and itself
-__device__ inline int64_t lane_scan(int64_t x, int lane)
+template <int CTRL, int ROW_MASK> __device__ inline int dpp_or_zero(int x)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d, 64);
-        if (lane >= d)
-            x += y;
-    }
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xf, false);
+}
+
+// sum over the wavefront's lanes before this one and itself
+__device__ inline int lane_scan(int x)
+{
+    x += dpp_or_zero<0x111, 0xf>(x);  // one lane up within the row of 16
+    x += dpp_or_zero<0x112, 0xf>(x);
+    x += dpp_or_zero<0x114, 0xf>(x);
+    x += dpp_or_zero<0x118, 0xf>(x);
+    x += dpp_or_zero<0x142, 0xa>(x);  // the last lane of rows 0 and 2 to rows 1 and 3
+    x += dpp_or_zero<0x143, 0xc>(x);  // the last lane of row 1 to rows 2 and 3
     return x;
+}
+
+// Tokens of a piece if `total` is cut into `budget` pieces.  (The total is a sum in fp32: the length is taken a little larger, so
+// that the pieces are not more.)
+__device__ inline int piece_tokens(float total, int budget, int align, int least)
+{
+    const float share = total * 1.0001f / (float)budget;
+    const int n = share < (float)PQ_MAX_TOKENS ? (int)share + 1 : PQ_MAX_TOKENS;
+    return n > least ? (n + align - 1) / align * align : least;
 }
 
 }  // namespace

@@ -16,10 +16,10 @@ struct work_place {
 };
 
 // Rows of sequence b that lie in the tensors
-__device__ inline int rows_there(const pq_paged_attn_args &a, int b, int &start)
+__device__ inline int rows_there(const pq_paged_attn_args &a, int b, int &start, int &asked)
 {
     start = a.tok_start[b];
-    const int n = a.tok_len[b];
+    const int n = asked = a.tok_len[b];
     if (start < 0 || start >= a.n_tokens || n <= 0)
         return 0;
     return n < a.n_tokens - start ? n : a.n_tokens - start;
@@ -32,83 +32,70 @@ struct work_rule {
     int budget;       // pieces that the keys of all tiles together are cut into at most, and a rest for each tile; 0: one a tile
 };
 
-__device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule, int b, int &start)
+__host__ __device__ inline work_rule few_rule(const pq_paged_prefill_plan &w)
 {
-    const int n = rows_there(a, b, start);
+    return work_rule{1, w.few_rows, PQ_PAGED_FEW_ROWS, w.few_budget};
+}
+
+__host__ __device__ inline work_rule tile_rule(const pq_paged_prefill_plan &w)
+{
+    return work_rule{w.few_rows + 1, INT32_MAX, PQ_PAGED_TILE_ROWS, w.tile_budget};
+}
+
+__device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule, int b, int &start, int &asked)
+{
+    const int n = rows_there(a, b, start, asked);
     return n * a.G >= rule.least && n * a.G <= rule.most ? n : 0;
 }
 
-// The list of a kernel's work: sequence after sequence, tile after tile (those that see most first), the pieces of a tile's
-// keys.  Finds the sequence for which `mine(entries before it, entries up to its end, first row, rows)` holds.
-template <typename F>
-__device__ inline bool find_sequence(const pq_paged_attn_args &a, const work_rule &rule, int lane, F mine, work_place &p, int &entries_before,
-                                     int &tiles, int &per_tile)
+// Entry e of the list of a kernel's work: sequence after sequence, tile after tile (those that see most first), the pieces of a
+// tile's keys.  BY_TILE: tile e instead, its first piece.
+template <bool BY_TILE = false>
+__device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &rule, int e, int lane, work_place &p)
 {
     const int tile_rows = rule.tile_rows, budget = rule.budget;
     p.keys = PQ_MAX_TOKENS;
     if (budget > 0) {
-        int64_t work = 0;
+        float work = 0.0f;
         for (int b0 = 0; b0 < a.n_seqs; b0 += 64)
             if (b0 + lane < a.n_seqs) {
-                int start;
-                const int n = (rows_of(a, rule, b0 + lane, start) * a.G + tile_rows - 1) / tile_rows;
-                work += (int64_t)n * paged_length(a.c, b0 + lane);
+                int start, asked;
+                const int n = (rows_of(a, rule, b0 + lane, start, asked) * a.G + tile_rows - 1) / tile_rows;
+                work += (float)n * (float)paged_length(a.c, b0 + lane);
             }
-        work = __shfl(lane_scan(work, lane), 63, 64);
-        const int64_t share = (work + budget - 1) / budget;
-        const int n = share < PQ_MAX_TOKENS ? (int)share : PQ_MAX_TOKENS;
-        p.keys = n > LEAST_KEYS ? (n + KEY_ALIGN - 1) / KEY_ALIGN * KEY_ALIGN : LEAST_KEYS;
+        p.keys = piece_tokens(wave_sum(work), budget, KEY_ALIGN, LEAST_KEYS);
     }
-    int before = 0;
+    int before = 0, tiles_before = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int start = 0, rows = 0, len = 0, splits = 1, n = 0;
+        int start = 0, asked = 0, rows = 0, len = 0, per_tile = 1, tiles = 0;
         if (b0 + lane < a.n_seqs) {
-            rows = rows_of(a, rule, b0 + lane, start);
+            rows = rows_of(a, rule, b0 + lane, start, asked);
             len = paged_length(a.c, b0 + lane);
-            splits = len > 0 ? (len + p.keys - 1) / p.keys : 1;
-            n = (rows * a.G + tile_rows - 1) / tile_rows * splits;
+            per_tile = len > 0 ? (len + p.keys - 1) / p.keys : 1;
+            tiles = (rows * a.G + tile_rows - 1) / tile_rows;
         }
-        const int upto = before + (int)lane_scan(n, lane);
-        const uint64_t found = __ballot(n > 0 && mine(upto - n, upto, start, rows));
+        const int n = tiles * per_tile, upto = before + lane_scan(n), tiles_upto = BY_TILE ? tiles_before + lane_scan(tiles) : 0;
+        const bool mine = BY_TILE ? e >= tiles_upto - tiles && e < tiles_upto : e >= upto - n && e < upto;
+        const uint64_t found = __ballot(mine);
         if (found != 0) {
             const int l = __builtin_ctzll(found);
             p.b = b0 + l;
             p.len = __builtin_amdgcn_readlane(len, l);
             p.first_row = __builtin_amdgcn_readlane(start, l);
             p.rows = __builtin_amdgcn_readlane(rows, l);
-            p.past = p.len - __builtin_amdgcn_readfirstlane(a.tok_len[p.b]);
-            per_tile = __builtin_amdgcn_readlane(splits, l);
-            tiles = __builtin_amdgcn_readlane(n, l) / per_tile;
-            entries_before = __builtin_amdgcn_readlane(upto - n, l);
+            p.past = p.len - __builtin_amdgcn_readlane(asked, l);
+            const int each = __builtin_amdgcn_readlane(per_tile, l), all = __builtin_amdgcn_readlane(tiles, l);
+            const int first = __builtin_amdgcn_readlane(upto - n, l);
+            const int from_end = BY_TILE ? e - __builtin_amdgcn_readlane(tiles_upto - tiles, l) : (e - first) / each;
+            p.tile = all - 1 - from_end;
+            p.split = BY_TILE ? 0 : e - first - from_end * each;
+            p.slot = first + from_end * each;
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
+        tiles_before = __builtin_amdgcn_readlane(tiles_upto, 63);
     }
     return false;
-}
-
-// entry e of the list
-__device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &rule, int e, int lane, work_place &p)
-{
-    int before, tiles, per_tile;
-    if (!find_sequence(a, rule, lane, [&](int from, int upto, int, int) { return e >= from && e < upto; }, p, before, tiles, per_tile))
-        return false;
-    p.tile = tiles - 1 - (e - before) / per_tile;
-    p.split = (e - before) % per_tile;
-    p.slot = e - p.split;
-    return true;
-}
-
-// the first piece of the tile that query head g (of its KV head) of row t of the tensors is in
-__device__ inline bool find_row(const pq_paged_attn_args &a, const work_rule &rule, int t, int g, int lane, work_place &p)
-{
-    int before, tiles, per_tile;
-    if (!find_sequence(a, rule, lane, [&](int, int, int start, int rows) { return t >= start && t - start < rows; }, p, before, tiles, per_tile))
-        return false;
-    p.tile = ((t - p.first_row) * a.G + g) / rule.tile_rows;
-    p.split = 0;
-    p.slot = before + (tiles - 1 - p.tile) * per_tile;
-    return true;
 }
 
 // A tile's rows of its sequence (token by token, query head by query head), and the pieces that the keys they see are in
