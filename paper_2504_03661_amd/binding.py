@@ -1,4 +1,4 @@
-"""Binding of libpq_attn.so: argument marshalling only — through ctypes, and for the two calls of a decoding step
+"""Binding of libpq_attn.so: argument marshalling only — through ctypes, and for the calls of a decoding step
 through a small extension module (csrc/pq_binding.cpp) that takes the same arguments apart natively, where that module
 has been built for this interpreter.
 
@@ -23,6 +23,7 @@ _LIB_PATH = os.path.join(_HERE, "libpq_attn.so")
 _lib = None
 _calls = None               # the extension module if there is one, and the addresses of its two functions in the library
 _decode_at = _append_at = 0
+_paged_at = {}              # the addresses of the paged cache's calls
 _CONTEXT = (int, ctypes.c_void_p, type(None))   # what the extension module takes as a context; ctypes decides on others
 
 
@@ -161,6 +162,8 @@ def load_library():
     _calls = calls
     _decode_at = ctypes.cast(L.pq_attn_decode, vp).value
     _append_at = ctypes.cast(L.pq_encode_append, vp).value
+    for name in ("plan", "append", "read", "decode", "prefill"):
+        _paged_at[name] = ctypes.cast(getattr(L, "pq_paged_" + name), vp).value
     _lib = L
     return L
 
@@ -332,39 +335,75 @@ def pq_paged_destroy(ctx: int) -> None:
     _check(load_library().pq_paged_destroy(ctx), "pq_paged_destroy")
 
 
-def pq_paged_plan(ctx, n_seqs, n_tokens, n_new, seq_len, free_list, free_count, block_table, new_seq_len, new_free_count,
-                  tok_start, tok_len, slot_map, stream=None) -> None:
-    _check(load_library().pq_paged_plan(ctx, int(n_seqs), int(n_tokens), _addr(n_new), _addr(seq_len), _addr(free_list),
-                                        _addr(free_count), _addr(block_table), _addr(new_seq_len), _addr(new_free_count),
-                                        _addr(tok_start), _addr(tok_len), _addr(slot_map), _stream(stream)), "pq_paged_plan")
+def pq_paged_plan(ctx, n_seqs, n_tokens, n_new, seq_len, free_list, free_count, block_table, new_seq_len,
+                       new_free_count, tok_start, tok_len, slot_map, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_plan(_paged_at["plan"], _current_stream, ctx, n_seqs, n_tokens, n_new, seq_len, free_list,
+                               free_count, block_table, new_seq_len, new_free_count, tok_start, tok_len, slot_map,
+                               stream)
+    else:
+        rc = L.pq_paged_plan(ctx, int(n_seqs), int(n_tokens), _addr(n_new), _addr(seq_len), _addr(free_list),
+                             _addr(free_count), _addr(block_table), _addr(new_seq_len), _addr(new_free_count),
+                             _addr(tok_start), _addr(tok_len), _addr(slot_map), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_plan")
 
 
-def pq_paged_append(ctx, n_tokens, new_k, new_v, kv_stride, slot_map, k_cache, v_cache, k_scale, v_scale, stream=None) -> None:
-    _check(load_library().pq_paged_append(ctx, int(n_tokens), _addr(new_k), _addr(new_v), int(kv_stride), _addr(slot_map),
-                                          _addr(k_cache), _addr(v_cache), _addr(k_scale), _addr(v_scale), _stream(stream)),
-           "pq_paged_append")
+def pq_paged_append(ctx, n_tokens, new_k, new_v, kv_stride, slot_map, k_cache, v_cache, k_scale, v_scale,
+                         stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_append(_paged_at["append"], _current_stream, ctx, n_tokens, new_k, new_v, kv_stride, slot_map,
+                                 k_cache, v_cache, k_scale, v_scale, stream)
+    else:
+        rc = L.pq_paged_append(ctx, int(n_tokens), _addr(new_k), _addr(new_v), int(kv_stride), _addr(slot_map),
+                               _addr(k_cache), _addr(v_cache), _addr(k_scale), _addr(v_scale), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_append")
 
 
 def pq_paged_read(ctx, n_seqs, n_rows, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, first, out_k, out_v,
-                  stream=None) -> None:
-    _check(load_library().pq_paged_read(ctx, int(n_seqs), int(n_rows), _addr(k_cache), _addr(v_cache), _addr(k_scale),
-                                        _addr(v_scale), _addr(block_table), _addr(seq_len), _addr(first), _addr(out_k),
-                                        _addr(out_v), _stream(stream)), "pq_paged_read")
+                       stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_read(_paged_at["read"], _current_stream, ctx, n_seqs, n_rows, k_cache, v_cache, k_scale,
+                               v_scale, block_table, seq_len, first, out_k, out_v, stream)
+    else:
+        rc = L.pq_paged_read(ctx, int(n_seqs), int(n_rows), _addr(k_cache), _addr(v_cache), _addr(k_scale),
+                             _addr(v_scale), _addr(block_table), _addr(seq_len), _addr(first), _addr(out_k),
+                             _addr(out_v), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_read")
 
 
 def pq_paged_decode(ctx, n_seqs, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, scale, out,
-                    stream=None) -> None:
-    _check(load_library().pq_paged_decode(ctx, int(n_seqs), _addr(q), int(q_stride), _addr(k_cache), _addr(v_cache),
-                                          _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len), float(scale),
-                                          _addr(out), _stream(stream)), "pq_paged_decode")
+                         stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_decode(_paged_at["decode"], _current_stream, ctx, n_seqs, q, q_stride, k_cache, v_cache,
+                                 k_scale, v_scale, block_table, seq_len, scale, out, stream)
+    else:
+        rc = L.pq_paged_decode(ctx, int(n_seqs), _addr(q), int(q_stride), _addr(k_cache), _addr(v_cache),
+                               _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len), float(scale),
+                               _addr(out), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_decode")
 
 
-def pq_paged_prefill(ctx, n_seqs, n_tokens, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, tok_start,
-                     tok_len, scale, out, stream=None) -> None:
-    _check(load_library().pq_paged_prefill(ctx, int(n_seqs), int(n_tokens), _addr(q), int(q_stride), _addr(k_cache),
-                                           _addr(v_cache), _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len),
-                                           _addr(tok_start), _addr(tok_len), float(scale), _addr(out), _stream(stream)),
-           "pq_paged_prefill")
+def pq_paged_prefill(ctx, n_seqs, n_tokens, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len,
+                          tok_start, tok_len, scale, out, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_prefill(_paged_at["prefill"], _current_stream, ctx, n_seqs, n_tokens, q, q_stride, k_cache,
+                                  v_cache, k_scale, v_scale, block_table, seq_len, tok_start, tok_len, scale, out,
+                                  stream)
+    else:
+        rc = L.pq_paged_prefill(ctx, int(n_seqs), int(n_tokens), _addr(q), int(q_stride), _addr(k_cache),
+                                _addr(v_cache), _addr(k_scale), _addr(v_scale), _addr(block_table), _addr(seq_len),
+                                _addr(tok_start), _addr(tok_len), float(scale), _addr(out), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_prefill")
 
 
 def pq_paged_device_error(ctx) -> int:

@@ -1,4 +1,4 @@
-// The per-step calls of the Python binding (pq_attn_decode, pq_encode_append) without ctypes: arguments are taken apart
+// The per-step calls of the Python binding (pq_attn_decode, pq_encode_append, the five of the paged cache) without ctypes: arguments are taken apart
 // here, the library's functions are called through the addresses that binding.py hands over.  A decoding step of one
 // short sequence (32 heads, 1K tokens) is bound by the host: with ctypes the two calls took 13 us of the step, marshalling
 // ten pointers each through Python helpers; with this module the step takes 16.1 us, before 22.8.
@@ -130,9 +130,81 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-PyMethodDef methods[] = {{"decode", (PyCFunction)(void (*)(void))decode, METH_FASTCALL, nullptr},
-                         {"append", (PyCFunction)(void (*)(void))append, METH_FASTCALL, nullptr},
-                         {nullptr, nullptr, 0, nullptr}};
+// The five calls of the paged cache: their arguments by kind, in the order of pq_attn.h (h context, p pointer, i int32, l int64,
+// f float; the stream comes last).
+constexpr int MOST = 16;
+
+union argument {
+    void *p;
+    int32_t i;
+    int64_t l;
+    float f;
+};
+
+// a: function address, current-stream callable, the arguments
+bool arguments(const char *kinds, PyObject *const *a, Py_ssize_t n, void **f, argument *to)
+{
+    const Py_ssize_t want = (Py_ssize_t)__builtin_strlen(kinds);
+    if (!count(n, want + 3) || !pointer(a[0], f))
+        return false;
+    for (Py_ssize_t k = 0; k < want; ++k) {
+        PyObject *o = a[2 + k];
+        uint64_t whole;
+        bool ok = true;
+        if (kinds[k] == 'h') {
+            ok = handle(o, &to[k].p);
+        } else if (kinds[k] == 'p') {
+            ok = pointer(o, &to[k].p);
+        } else if (kinds[k] == 'f') {
+            PyObject *number = PyNumber_Float(o);
+            ok = number != nullptr;
+            if (ok) {
+                to[k].f = (float)PyFloat_AS_DOUBLE(number);
+                Py_DECREF(number);
+            }
+        } else {
+            ok = integer(o, &whole);
+            if (ok && kinds[k] == 'i')
+                to[k].i = (int32_t)(uint32_t)whole;
+            else if (ok)
+                to[k].l = (int64_t)whole;
+        }
+        if (!ok)
+            return false;
+    }
+    return stream(a[2 + want], a[1], &to[want].p);
+}
+
+#define PAGED_CALL(NAME, KINDS, TYPE, CALL)                                          \
+    PyObject *NAME(PyObject *, PyObject *const *args, Py_ssize_t n)                  \
+    {                                                                                \
+        void *f;                                                                     \
+        argument a[MOST];                                                            \
+        if (!arguments(KINDS, args, n, &f, a))                                       \
+            return nullptr;                                                          \
+        int rc;                                                                      \
+        Py_BEGIN_ALLOW_THREADS                                                       \
+        rc = ((int (*)TYPE)f)CALL;                                                   \
+        Py_END_ALLOW_THREADS                                                         \
+        return PyLong_FromLong(rc);                                                  \
+    }
+
+typedef void *P;
+PAGED_CALL(paged_plan, "hiipppppppppp", (P, int32_t, int32_t, P, P, P, P, P, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].i, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p, a[13].p))
+PAGED_CALL(paged_append, "hipplppppp", (P, int32_t, P, P, int64_t, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].p, a[4].l, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p))
+PAGED_CALL(paged_read, "hiippppppppp", (P, int32_t, int32_t, P, P, P, P, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].i, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p))
+PAGED_CALL(paged_decode, "hiplppppppfp", (P, int32_t, P, int64_t, P, P, P, P, P, P, float, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].l, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].f, a[11].p, a[12].p))
+PAGED_CALL(paged_prefill, "hiiplppppppppfp", (P, int32_t, int32_t, P, int64_t, P, P, P, P, P, P, P, P, float, P, P),
+           (a[0].p, a[1].i, a[2].i, a[3].p, a[4].l, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p, a[13].f,
+            a[14].p, a[15].p))
+
+#define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {METHOD(decode), METHOD(append), METHOD(paged_plan), METHOD(paged_append), METHOD(paged_read),
+                         METHOD(paged_decode), METHOD(paged_prefill), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pq_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

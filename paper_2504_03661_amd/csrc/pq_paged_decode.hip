@@ -21,6 +21,7 @@ namespace {
 
 constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = 16;
 constexpr int STEP = 32;                // tokens a wavefront takes at a time
+constexpr int AT_ONCE = 16;             // partials of a row on their way together
 constexpr int CHUNK_ALIGN = WAVES * STEP;
 
 // Two pieces of 16 tokens as they lie in memory, and their blocks' scales
@@ -303,15 +304,24 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     for (int i = threadIdx.x; i < rows * (D / 2); i += THREADS) {
         const int r = i / (D / 2), d = i % (D / 2) * 2;
         float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
-#pragma unroll 4
-        for (int c = 0; c < p.chunks; ++c) {
-            const float2 ml = fetch(parts + (int64_t)c * per_chunk + r * (D + 2));
-            const float2 v = fetch(parts + (int64_t)c * per_chunk + r * (D + 2) + 2 + d);
-            const float high = fmaxf(top, ml.x), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
-            top = high;
-            sum = fmaf(ml.y, by, sum * old);
-            x = fmaf(v.x, by, x * old);
-            y = fmaf(v.y, by, y * old);
+        const float *from = parts + r * (D + 2);
+        for (int c0 = 0; c0 < p.chunks; c0 += AT_ONCE, from += (int64_t)AT_ONCE * per_chunk) {
+            float2 ml[AT_ONCE], v[AT_ONCE];
+#pragma unroll
+            for (int c = 0; c < AT_ONCE; ++c) {
+                const float *piece = from + (c0 + c < p.chunks ? c : 0) * per_chunk;
+                ml[c] = fetch(piece);
+                v[c] = fetch(piece + 2 + d);
+            }
+#pragma unroll
+            for (int c = 0; c < AT_ONCE; ++c) {
+                const float m_c = c0 + c < p.chunks ? ml[c].x : -INFINITY;  // (a repeated one counts for nothing)
+                const float high = fmaxf(top, m_c), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(m_c - high);
+                top = high;
+                sum = fmaf(ml[c].y, by, sum * old);
+                x = fmaf(v[c].x, by, x * old);
+                y = fmaf(v[c].y, by, y * old);
+            }
         }
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         out[r * D + d] = paged_elem<T>::down(x * by);
@@ -321,11 +331,12 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
 
 }  // namespace
 
-// Chunks are as many as keep the chip busy (PER_CU workgroups a compute unit), not more than a merge reads in a few
-// microseconds.
+// Chunks are as many as keep the chip busy, PER_CU workgroups a compute unit (8 x 32 heads x 32K: 348 us with one, 336 with two,
+// 342 with three; 32 query / 8 KV heads x 128K 53, 54 and 59), and not more than the last workgroup reads in a few
+// microseconds (16 query heads of one KV head x 100K: 46 us with up to 128, 40 with 64).
 pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu)
 {
-    constexpr int PER_CU = 2, MOST = 128;
+    constexpr int PER_CU = 2, MOST = 64;
     pq_paged_decode_plan w;
     const int G = cfg->n_q_heads / cfg->n_kv_heads;
     w.n_sub = (G + ROWS - 1) / ROWS;
