@@ -313,7 +313,8 @@ int pq_paged_plan(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const int
  *
  * The slots of one block are those of rows in a row, ascending by one, as pq_paged_plan gives them (a block that is written
  * from two places of the map, or a slot that comes twice, leaves that block's contents unspecified, no other's).  Tokens of
- * the block in front of the first such slot are older ones and are kept; a block whose slot 0 is written begins anew.
+ * the block in front of the first such slot are older ones and are kept, those behind the last are not; a block whose slot 0 is
+ * written begins anew.
  * 0 <= n_tokens <= max_tokens; 0 does nothing. */
 int pq_paged_append(pq_paged_ctx *ctx, int32_t n_tokens, const void *new_k, const void *new_v, int64_t kv_stride,
                     const int32_t *slot_map, uint8_t *k_cache, uint8_t *v_cache, float *k_scale, float *v_scale,

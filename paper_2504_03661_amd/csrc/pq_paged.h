@@ -38,17 +38,8 @@ struct pq_paged_ctx {
     int n_cu;
     pq_paged_decode_plan decode;
     pq_paged_prefill_plan prefill;
-    int *plan;              // scratch of pq_paged_plan: PQ_PAGED_PLAN_ARRAYS arrays of max_seqs + 1
+    int *plan;              // scratch of pq_paged_plan: what its two launches hand over
     unsigned int *dev_err;  // sticky error word
-};
-
-// per-sequence numbers between the two halves of pq_paged_plan
-enum {
-    PQ_PAGED_PLAN_OLD,    // length before
-    PQ_PAGED_PLAN_FREED,  // blocks given back by the requests before this one
-    PQ_PAGED_PLAN_TAKEN,  // blocks taken by the requests before this one
-    PQ_PAGED_PLAN_COUNTS, // [0] free blocks before the call, [1] after the pushes
-    PQ_PAGED_PLAN_ARRAYS
 };
 
 // a cache as the kernels see it
@@ -67,7 +58,6 @@ struct pq_paged_plan_args {
     const int32_t *free_count;
     int32_t *table, *new_seq_len, *new_free_count, *tok_start, *tok_len, *slot_map;
     int *scratch;
-    int scratch_stride;
     int n_seqs, n_tokens, n_blocks, max_blocks, log_block;
     unsigned int *dev_err;
 };
@@ -99,6 +89,7 @@ struct pq_paged_attn_args {
     int n_seqs, n_tokens, Hq, G;
 };
 
+int64_t pq_paged_plan_scratch_bytes();
 hipError_t pq_launch_paged_plan(const pq_paged_ctx *ctx, const pq_paged_plan_args &a, hipStream_t s);
 hipError_t pq_launch_paged_append(const pq_paged_ctx *ctx, const pq_paged_append_args &a, hipStream_t s);
 hipError_t pq_launch_paged_read(const pq_paged_ctx *ctx, const pq_paged_read_args &a, hipStream_t s);

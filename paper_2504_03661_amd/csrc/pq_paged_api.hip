@@ -146,7 +146,7 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     ctx->cfg = *cfg;
     ctx->log_block = cfg->block_tokens == 16 ? 4 : cfg->block_tokens == 32 ? 5 : 6;
     ctx->n_cu = n_cu;
-    const size_t plan_bytes = (size_t)PQ_PAGED_PLAN_ARRAYS * (cfg->max_seqs + 1) * sizeof(int);
+    const size_t plan_bytes = (size_t)pq_paged_plan_scratch_bytes();
     ctx->decode = pq_paged_plan_decode(cfg, n_cu);
     const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
     const size_t part_bytes = (size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float);
@@ -216,7 +216,6 @@ int pq_paged_plan(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const int
     a.tok_len = tok_len;
     a.slot_map = slot_map;
     a.scratch = ctx->plan;
-    a.scratch_stride = ctx->cfg.max_seqs + 1;
     a.n_seqs = n_seqs;
     a.n_tokens = n_tokens;
     a.n_blocks = ctx->cfg.n_blocks;

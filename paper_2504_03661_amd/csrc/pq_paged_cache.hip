@@ -3,6 +3,7 @@
 
 #include <cfloat>
 
+#include "pq_device_utils.h"
 #include "pq_paged.h"
 
 namespace {
@@ -40,16 +41,72 @@ __device__ inline uint32_t wave_max_u32(uint32_t x)
     return x;
 }
 
-// One wavefront writes the tokens that a call brings to one block, for one KV head and K or V: it needs no other's results.
-// A lane has four tokens by eight dims of a piece of 16 tokens — the four tokens are the bytes of V's words, the eight dims
-// one load of a row.
-//   A wavefront looks at `span` rows of the slot map and takes up every run that begins there.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void pq_paged_append_kernel(pq_paged_append_args a, int span, int n_spans)
+// Largest |x| of values as bits, in which NaN is larger than any number; two 16-bit types a word at a time.
+template <typename T> struct largest_bits {
+    typedef uint16_t pair __attribute__((ext_vector_type(2)));
+    pair high = {0, 0};
+    __device__ void add(const paged_row8<T> &r)
+    {
+        uint4 w;
+        __builtin_memcpy(&w, &r, sizeof(w));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = comp(w, i) & 0x7fff7fffu;
+            high = __builtin_elementwise_max(high, __builtin_bit_cast(pair, bits));
+        }
+    }
+    __device__ float all() const
+    {
+        const uint16_t bits = (uint16_t)wave_max_u32(high.x > high.y ? high.x : high.y);
+        return paged_elem<T>::up(__builtin_bit_cast(T, bits));
+    }
+};
+template <> struct largest_bits<float> {
+    uint32_t high = 0;
+    __device__ void add(const paged_row8<float> &r)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(r.x[i]) & 0x7fffffffu;
+            high = bits > high ? bits : high;
+        }
+    }
+    __device__ float all() const { return __uint_as_float(wave_max_u32(high)); }
+};
+
+// Stored bytes of 8 values as whole numbers in fp32, x / s + 128 rounded.  In one fma the quotient is at most 2^-15 off: where none
+// of the eight is that near a tie they are right as they are, else (one group of a wavefront's in thirty) all are decided exactly.
+template <typename T> __device__ inline void stored8(const paged_row8<T> &row, float s, float inv, float *out)
 {
-    constexpr int GROUPS = D / 8, LANES = 4 * GROUPS, PIECES = 64 / LANES;  // lanes of a piece, pieces at a time
-    const int lane = threadIdx.x & 63;
-    const int unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
+    float far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float y = fmaf(paged_elem<T>::up(row.x[e]), inv, 128.0f);
+        out[e] = rintf(y);
+        far = fmaxf(far, fabsf(y - out[e]));
+    }
+    if (far > 0.5f - 0x1p-15f)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            out[e] = nearest_code(paged_elem<T>::up(row.x[e]), s, inv) + 128.0f;
+}
+
+// PER wavefronts write the tokens that a call brings to one block, for one KV head and K or V: they need no others' results.
+// Each has a piece of the block, 16 tokens (two pieces of 64 dims), and a lane of it four tokens by eight dims — the four tokens
+// are the bytes of V's words, the eight dims one load of a row —, kept from the search for the largest to the rounding: a
+// value is read once.  V's words go through LDS, from where they leave 16 bytes a lane in a row.  A unit of wavefronts looks
+// at `span` rows of the slot map and takes up every run that begins there.
+//   Bound by HBM: a value is 2 or 4 bytes read and one written.  32K tokens x 32 heads in fp16 at 16 tokens a block: 318 us where
+// the rows were read twice and V's words stored 4 bytes at a time, 250 us without that, 210 us with the slots read in one go.
+template <typename T, int D, int PER>
+__global__ __launch_bounds__(PER == 1 ? 256 : 64 * PER) void pq_paged_append_kernel(pq_paged_append_args a, int span, int n_spans)
+{
+    constexpr int GROUPS = D / 8, LANES = 4 * GROUPS, PIECES = 64 / LANES;  // lanes of a piece, pieces of a wavefront
+    constexpr int UNITS = PER == 1 ? 4 : 1;                                  // of a workgroup
+    __shared__ uint32_t words_of[UNITS * PER][PIECES][4 * D];                // V's words of a wavefront's pieces
+    __shared__ uint32_t largest_of[2][PER];  // (as bits: a NaN is the largest)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int unit = blockIdx.x * UNITS + wave / PER, member = wave % PER;
     const int kind = unit & 1, h = (unit >> 1) % a.Hkv, part = (unit >> 1) / a.Hkv;
     if (part >= n_spans)
         return;
@@ -57,45 +114,54 @@ __global__ __launch_bounds__(256) void pq_paged_append_kernel(pq_paged_append_ar
     const T *x = (const T *)a.x[kind] + (int64_t)h * D;
     const int t0 = part * span;
 
-    bool begins = false;
-    if (lane < span && t0 + lane < a.n_tokens) {
-        const int t = t0 + lane, now = a.slot[t], before = t > 0 ? a.slot[t - 1] : -2;
-        if (now >= n_slots)
-            paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
-        else
-            begins = now >= 0 && (before != now - 1 || (now & (block_tokens - 1)) == 0);
+    // the rows' slots, and behind them those that a run may go on in: all that the search for runs needs, in one go
+    const auto slot_of = [&](int t) { return t < a.n_tokens ? a.slot[t] : -2; };
+    const int here = slot_of(t0 + lane), beyond = span > 1 && block_tokens == 64 ? slot_of(t0 + 64 + lane) : -2;
+    int before = __shfl_up(here, 1, 64);
+    if (lane == 0)
+        before = t0 > 0 ? a.slot[t0 - 1] : -2;
+    bool begins = lane < span && here >= 0 && (before != here - 1 || (here & (block_tokens - 1)) == 0);
+    if (begins && here >= n_slots) {
+        begins = false;
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
     }
     uint64_t runs = __ballot(begins);
-    const int piece0 = lane / LANES, quad = lane % LANES / GROUPS, d0 = lane % GROUPS * 8;
-    while (runs != 0) {
-        const int t = t0 + __builtin_ctzll(runs);
+    const int p = member * PIECES + lane / LANES, quad = lane % LANES / GROUPS, d0 = lane % GROUPS * 8, r0 = p * 16 + quad * 4;
+    for (int turn = 0; runs != 0; turn ^= 1) {
+        const int first = __builtin_ctzll(runs), t = t0 + first;
         runs &= runs - 1;
-        const int slot = __builtin_amdgcn_readfirstlane(a.slot[t]);
+        const int slot = __builtin_amdgcn_readlane(here, first);
         const int block = slot >> a.log_block, from = slot & (block_tokens - 1);
-        const bool follows = lane < block_tokens - from && t + lane < a.n_tokens && a.slot[t + lane] == slot + lane;
+        const int same = __shfl(here, (first + lane) & 63, 64), later = __shfl(beyond, (first + lane) & 63, 64);
+        const bool follows = lane < block_tokens - from && (first + lane < 64 ? same : later) == slot + lane;
         const uint64_t stops = ~__ballot(follows);
         const int n = stops != 0 ? __builtin_ctzll(stops) : 64;
         const int upto = from + n;  // tokens [from, upto) of the block are new, those before are older
 
-        // the largest |x|; as bits, so that a NaN is larger than any number
-        uint32_t high = 0;
-        for (int p = piece0 + (from >> 4) / PIECES * PIECES; p * 16 < upto; p += PIECES)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = p * 16 + quad * 4 + i;
-                if (r < from || r >= upto)
-                    continue;
-                float v[8];
-                paged_load8(x + (int64_t)(t + r - from) * a.stride + d0, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t bits = __float_as_uint(v[e]) & 0x7fffffffu;
-                    high = bits > high ? bits : high;
-                }
-            }
-        const float largest = __uint_as_float(wave_max_u32(high));
         float *const scale_at = a.scale[kind] + (int64_t)block * a.Hkv + h;
         const float was = from > 0 ? *scale_at : 0.0f;
+        paged_row8<T> rows[4];
+        largest_bits<T> high;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r0 + i >= from && r0 + i < upto)
+                rows[i] = *(const paged_row8<T> *)(x + (int64_t)(t + r0 + i - from) * a.stride + d0);
+            else
+                rows[i] = paged_row8<T>{};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            high.add(rows[i]);
+        float largest = high.all();
+        if constexpr (PER > 1) {
+            if (lane == 0)
+                largest_of[turn][member] = __float_as_uint(largest);
+            __syncthreads();  // (also: everybody has read the block's scale before it is written, below)
+            uint32_t bits = 0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                bits = largest_of[turn][i] > bits ? largest_of[turn][i] : bits;
+            largest = __uint_as_float(bits);
+        }
         float s;
         if (!(largest <= FLT_MAX) || !(was <= FLT_MAX))
             s = __uint_as_float(0x7fc00000u);  // (codes 0)
@@ -105,80 +171,78 @@ __global__ __launch_bounds__(256) void pq_paged_append_kernel(pq_paged_append_ar
         const float inv = finite ? 1.0f / s : 0.0f;
 
         uint8_t *const bytes = a.cache[kind] + ((int64_t)block * a.Hkv + h) * ((int64_t)D << a.log_block);
-        const int first_piece = grown ? 0 : (from >> 4) / PIECES * PIECES;
-        for (int p = piece0 + first_piece; p * 16 < upto; p += PIECES) {
-            const int r0 = p * 16 + quad * 4;
-            const bool some = r0 < upto && (grown || r0 + 4 > from);
-            if (!some)
-                continue;
-            // codes of the 4 tokens' 8 dims as bytes, a word per dim; those that are not written keep what is there
-            uint32_t words[8];
-            const bool whole = r0 >= from && r0 + 4 <= upto;
-            if (!whole) {
-                if (kind == 0) {
-                    uint2 rows[4];
+        if (grown)  // (rare, and kept small: unrolled it took half of the registers)
+#pragma unroll 1
+            for (int k = 0; k < 8 && r0 < from; ++k) {
+                uint32_t *const at = (uint32_t *)(bytes + (kind == 0 ? (r0 + k / 2) * D + d0 + k % 2 * 4 : pq_paged_v_offset(r0, d0 + k, D)));
+                if (kind == 0 && r0 + k / 2 >= from)
+                    break;
+                const uint32_t old = *at;
+                uint32_t w = old;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        rows[i] = *(const uint2 *)(bytes + (r0 + i) * D + d0);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        words[e] = 0;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            words[e] |= (((e < 4 ? rows[i].x : rows[i].y) >> (8 * (e & 3))) & 0xffu) << (8 * i);
+                for (int i = 0; i < 4; ++i)
+                    if (kind == 0 || r0 + i < from) {
+                        const int c = (int)((old >> (8 * i)) & 0xffu) - 128;
+                        w = (w & ~(0xffu << (8 * i))) | (stored(regrown_code(c, was, s)) << (8 * i));
                     }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        words[e] = *(const uint32_t *)(bytes + pq_paged_v_offset(r0, d0 + e, D));
-                }
-                if (grown)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (r0 + i < from)
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                const int c = (int)((words[e] >> (8 * i)) & 0xffu) - 128;
-                                words[e] = (words[e] & ~(0xffu << (8 * i))) | (stored(regrown_code(c, was, s)) << (8 * i));
-                            }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    words[e] = 0;
+                *at = w;
             }
+        if (kind == 0) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = r0 + i;
                 if (r < from || r >= upto)
                     continue;
-                float v[8];
-                paged_load8(x + (int64_t)(t + r - from) * a.stride + d0, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int c = finite ? (int)nearest_code(v[e], s, inv) : 0;
-                    words[e] = (words[e] & ~(0xffu << (8 * i))) | (stored(c) << (8 * i));
-                }
-            }
-            if (kind == 0) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (r0 + i >= upto)
-                        continue;
-                    uint2 row = make_uint2(0, 0);
+                uint2 w = make_uint2(0x80808080u, 0x80808080u);
+                if (finite) {
+                    float b[8];
+                    stored8<T>(rows[i], s, inv, b);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        row.x |= ((words[e] >> (8 * i)) & 0xffu) << (8 * e);
-                        row.y |= ((words[e + 4] >> (8 * i)) & 0xffu) << (8 * e);
+                        w.x = __builtin_amdgcn_cvt_pk_u8_f32(b[e], e, w.x);
+                        w.y = __builtin_amdgcn_cvt_pk_u8_f32(b[e + 4], e, w.y);
                     }
-                    *(uint2 *)(bytes + (r0 + i) * D + d0) = row;
                 }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    *(uint32_t *)(bytes + pq_paged_v_offset(r0, d0 + e, D)) = words[e];
+                *(uint2 *)(bytes + r * D + d0) = w;
             }
+        } else {
+            // quads of four tokens with new ones among them; an older token beside them keeps its byte
+            const auto written = [&](int r) { return r < upto && r + 4 > from; };
+            uint32_t words[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                words[e] = 0x80808080u;
+            if (written(r0)) {
+                if (r0 < from)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        words[e] = *(const uint32_t *)(bytes + pq_paged_v_offset(r0, d0 + e, D));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (r0 + i >= from && r0 + i < upto) {
+                        float b[8];
+                        if (finite)
+                            stored8<T>(rows[i], s, inv, b);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            words[e] = __builtin_amdgcn_cvt_pk_u8_f32(finite ? b[e] : 128.0f, i, words[e]);
+                    }
+            }
+            uint32_t *const room = words_of[wave][lane / LANES];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                room[pq_paged_v_offset(quad * 4, d0 + e, D) / 4] = words[e];
+            __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS operations are in order)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int chunk = k * LANES + lane % LANES;  // 16 bytes of one quad: four tokens, four dims
+                const uint4 w = ((const uint4 *)room)[chunk];
+                if (written(p * 16 + chunk % 64 / 16 * 4))
+                    *(uint4 *)(bytes + p * (16 * D) + chunk * 16) = w;
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        if (lane == 0)
+        if (lane == 0 && member == 0)
             *scale_at = s;
     }
 }
@@ -243,14 +307,36 @@ template <typename T, int D> __global__ __launch_bounds__(256) void pq_paged_rea
 
 }  // namespace
 
+namespace {
+
+template <typename T, int D, int PER> void launch_append(const pq_paged_append_args &a, int span, int n_spans, hipStream_t s)
+{
+    const int64_t units = n_spans * 2 * (int64_t)a.Hkv;
+    const dim3 grid((unsigned)(PER == 1 ? (units + 3) / 4 : units)), threads(PER == 1 ? 256 : 64 * PER);
+    hipLaunchKernelGGL((pq_paged_append_kernel<T, D, PER>), grid, threads, 0, s, a, span, n_spans);
+}
+
+template <typename T, int D> void launch_append(int block_tokens, const pq_paged_append_args &a, int span, int n_spans, hipStream_t s)
+{
+    const int per = block_tokens * D / 2048;  // (16 tokens of 64 dims: half a wavefront)
+    if constexpr (D == 128)
+        if (per == 4)
+            return launch_append<T, D, 4>(a, span, n_spans, s);
+    if (per == 2)
+        launch_append<T, D, 2>(a, span, n_spans, s);
+    else
+        launch_append<T, D, 1>(a, span, n_spans, s);
+}
+
+}  // namespace
+
+// A unit a row (of K or V of a head) where there are few, so that the blocks of a step's many sequences are written side by
+// side; else a unit a block's worth of rows, most of which begin no run.
 hipError_t pq_launch_paged_append(const pq_paged_ctx *ctx, const pq_paged_append_args &a, hipStream_t s)
 {
-    const int64_t per_row = 2 * (int64_t)a.Hkv;
-    const int span = a.n_tokens * per_row <= 64 * (int64_t)ctx->n_cu ? 1 : ctx->cfg.block_tokens;
+    const int span = a.n_tokens * 2 * (int64_t)a.Hkv <= 64 * (int64_t)ctx->n_cu ? 1 : ctx->cfg.block_tokens;
     const int n_spans = (a.n_tokens + span - 1) / span;
-    const int64_t units = n_spans * per_row;
-#define LAUNCH(T, D) \
-    hipLaunchKernelGGL((pq_paged_append_kernel<T, D>), dim3((unsigned)((units + 3) / 4)), dim3(256), 0, s, a, span, n_spans)
+#define LAUNCH(T, D) launch_append<T, D>(ctx->cfg.block_tokens, a, span, n_spans, s)
     PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);
 #undef LAUNCH
     return hipGetLastError();

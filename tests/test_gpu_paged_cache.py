@@ -198,6 +198,22 @@ def test_append_of_ties_small_numbers_and_what_is_not_finite():
         np.testing.assert_array_equal(got.codes[1, :, :3], store.model[i].codes[1, :, :3])
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("dim,block", [(128, 16), (128, 32), (128, 64), (64, 32), (64, 64)])
+def test_one_value_that_is_not_finite_anywhere_in_a_block(dtype, dim, block):
+    """In every piece of the block, first and last, with larger and smaller numbers in the others."""
+    rng = np.random.default_rng(dim + block)
+    places = [0, 1, block // 2 - 1, block // 2, block - 1] + [16 * i + 5 for i in range(block // 16)]
+    store = Store(dtype, len(places), dim, block, 2)
+    xs = draw(rng, block, len(places), dim)
+    for h, r in enumerate(places):
+        xs[0][r, h, rng.integers(dim)] = [np.nan, np.inf, -np.inf][h % 3]
+        xs[1][r, h, rng.integers(dim)] = [-np.inf, np.nan, np.nan][h % 3]
+    store.append(xs, np.arange(block) + block)
+    store.check()
+    assert np.isnan(store.model[0].scale[1]).all()
+
+
 def test_append_outside_the_cache_writes_nothing():
     rng = np.random.default_rng(6)
     store = Store("f16", 2, 128, 16, 3)
