@@ -272,7 +272,8 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_pag
     if (!find_work<true>(a, rule, blockIdx.y / a.c.Hkv, lane, p))
         return;
     const tile_place tile(p, a.G, TILE_ROWS);
-    if (tile.pieces == 1)
+    // (more pieces than slots: sequences whose rows overlap, of which the list of work is longer than the grid)
+    if (tile.pieces == 1 || p.slot + tile.pieces > slots)
         return;
     const int d = 2 * (lane % (D / 2)), first = (blockIdx.x * MERGE_WAVES + wave) * EACH;
     for (int r = first; r < first + EACH && r < tile.rows; ++r) {

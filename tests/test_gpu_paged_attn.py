@@ -260,6 +260,20 @@ def test_prefill_keeps_to_the_rows_it_has(start, count):
             check(out[part], *c.attention(values[part], b, 0.1, 64 - count[b] + 1 + np.arange(count[b])), "f16", 64)
 
 
+def test_sequences_whose_rows_overlap_stay_within_memory():
+    """What comes out is nobody's, but no row outside is written and the next call is right."""
+    rng = np.random.default_rng(25)
+    c = Filled(rng, np.array([3000] * 60), 2, 64, 16)
+    ctx = context("f16", 4, 2, 64, 16, c.n_blocks, c.width, 60, 40)
+    q, values = queries(rng, 40, 4, 64, "f16")
+    room = torch.full((48, 4, 64), 7.0, dtype=torch.float16, device="cuda")
+    pq.pq_paged_prefill(ctx.handle, 60, 40, q, q.shape[1], *c.args(), dev([0] * 61), dev([40] * 60), 0.1, room[4:44])
+    torch.cuda.synchronize()
+    assert (room[:4] == 7.0).all() and (room[44:] == 7.0).all()
+    pq.pq_paged_prefill(ctx.handle, 1, 40, q, q.shape[1], *c.args(), dev([0, 40]), dev([40]), 0.1, room[4:44])
+    check(room[4:44], *c.attention(values, 0, 0.1, 2961 + np.arange(40)), "f16", 64)
+
+
 def test_a_cache_of_more_than_4_gib():
     """Offsets beyond 32 bits: blocks at the far end of a cache of 4.5 GiB a tensor."""
     Hkv, dim, block = 32, 128, 64
