@@ -72,12 +72,7 @@ pq_paged_view view(const pq_paged_ctx *ctx, const uint8_t *k, const uint8_t *v, 
 
 void free_ctx(pq_paged_ctx *ctx)
 {
-    if (ctx->decode.partials) (void)hipFree(ctx->decode.partials);
-    if (ctx->decode.tickets) (void)hipFree(ctx->decode.tickets);
-    if (ctx->prefill.tile_partials) (void)hipFree(ctx->prefill.tile_partials);
-    if (ctx->prefill.few_partials) (void)hipFree(ctx->prefill.few_partials);
-    if (ctx->plan) (void)hipFree(ctx->plan);
-    if (ctx->dev_err) (void)hipFree(ctx->dev_err);
+    (void)hipFree(ctx->scratch);
     delete ctx;
 }
 
@@ -146,29 +141,30 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     ctx->cfg = *cfg;
     ctx->log_block = cfg->block_tokens == 16 ? 4 : cfg->block_tokens == 32 ? 5 : 6;
     ctx->n_cu = n_cu;
-    const size_t plan_bytes = (size_t)pq_paged_plan_scratch_bytes();
     ctx->decode = pq_paged_plan_decode(cfg, n_cu);
-    const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
-    const size_t part_bytes = (size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float);
     ctx->prefill = pq_paged_plan_prefill(cfg, n_cu);
-    const size_t tile_bytes = (size_t)pq_paged_prefill_partials(cfg, ctx->prefill, false) * sizeof(float);
-    const size_t few_bytes = (size_t)pq_paged_prefill_partials(cfg, ctx->prefill, true) * sizeof(float);
-    bool ok = hipMalloc((void **)&ctx->plan, plan_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->prefill.tile_partials, tile_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->prefill.few_partials, few_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->decode.partials, part_bytes) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->decode.tickets, slots * sizeof(unsigned int)) == hipSuccess;
-    ok = ok && hipMalloc((void **)&ctx->dev_err, sizeof(unsigned int)) == hipSuccess;
-    if (!ok) {
+    // one allocation: what has to be zero first, then the rest
+    const int64_t slots = pq_paged_decode_slots(cfg, ctx->decode);
+    size_t bytes = 0;
+    const auto room = [&](size_t n) { const size_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
+    const size_t err_at = room(sizeof(unsigned int)), tickets_at = room(slots * sizeof(unsigned int));
+    const size_t zeros = bytes;
+    const size_t plan_at = room((size_t)pq_paged_plan_scratch_bytes());
+    const size_t decode_at = room((size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float));
+    const size_t tile_at = room((size_t)cfg->n_kv_heads * ctx->prefill.tile_room * sizeof(float));
+    const size_t few_at = room((size_t)cfg->n_kv_heads * ctx->prefill.few_room * sizeof(float));
+    if (hipMalloc((void **)&ctx->scratch, bytes) != hipSuccess) {
         (void)hipGetLastError();
-        free_ctx(ctx);
+        delete ctx;
         return PQ_ERR_ALLOC;
     }
-    ok = hipMemset(ctx->plan, 0, plan_bytes) == hipSuccess;
-    ok = ok && hipMemset(ctx->decode.tickets, 0, slots * sizeof(unsigned int)) == hipSuccess;
-    ok = ok && hipMemset(ctx->dev_err, 0, sizeof(unsigned int)) == hipSuccess;
-    ok = ok && hipDeviceSynchronize() == hipSuccess;
-    if (!ok) {
+    ctx->dev_err = (unsigned int *)(ctx->scratch + err_at);
+    ctx->decode.tickets = (unsigned int *)(ctx->scratch + tickets_at);
+    ctx->plan = (int *)(ctx->scratch + plan_at);
+    ctx->decode.partials = (float *)(ctx->scratch + decode_at);
+    ctx->prefill.tile_partials = (float *)(ctx->scratch + tile_at);
+    ctx->prefill.few_partials = (float *)(ctx->scratch + few_at);
+    if (hipMemset(ctx->scratch, 0, zeros) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
         (void)hipGetLastError();
         free_ctx(ctx);
         return PQ_ERR_HIP;

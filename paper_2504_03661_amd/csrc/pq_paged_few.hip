@@ -236,7 +236,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
         row_l[r] = sum;
     }
     __syncthreads();
-    float *const to = w.few_partials + ((int64_t)h * w.few_slots + p.slot + p.split) * (ROWS * (D + 2));
+    float *const to = w.few_partials + h * w.few_room + (int64_t)(p.slot + p.split) * (ROWS * (D + 2));
     for (int i = threadIdx.x; i < tile.rows * (D / 2); i += THREADS) {
         const int r = i / (D / 2), d = i % (D / 2) * 2;
         float x = 0.0f, y = 0.0f;
@@ -259,32 +259,46 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     }
 }
 
-// Puts the pieces of a tile's keys together, a wavefront for EACH rows, one after another, and two dims a lane.
+// The merge of both kernels' tiles in one launch: tiles are [few, whole or half], a workgroup has MERGE_WAVES times `each` rows.
+struct merge_part {
+    work_rule rule;
+    const float *partials;
+    int64_t room;
+    int tiles, groups, each;  // tiles that there can be, workgroups of a tile
+};
+
 constexpr int MERGE_WAVES = 4;
 
-template <typename T, int D, int TILE_ROWS, int EACH>
-__global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_paged_attn_args a, work_rule rule, const float *partials, int slots)
+// Puts the pieces of a tile's keys together, a wavefront for some rows, one after another, and two dims a lane.
+template <typename T, int D>
+__global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_paged_attn_args a, merge_part few, merge_part many)
 {
-    constexpr int STRIDE = TILE_ROWS * (D + 2);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int h = blockIdx.y % a.c.Hkv;
+    const int few_groups = few.tiles * few.groups * a.c.Hkv;
+    const bool is_few = (int)blockIdx.x < few_groups;
+    const int at = is_few ? blockIdx.x : blockIdx.x - few_groups;
+    const merge_part &part = is_few ? few : many;
+    const int group = at % part.groups, h = at / part.groups % a.c.Hkv;
+    const float *const partials = part.partials;
+    const int64_t room = part.room;
     work_place p;
-    if (!find_work<true>(a, rule, blockIdx.y / a.c.Hkv, lane, p))
+    if (!find_work<true>(a, part.rule, at / part.groups / a.c.Hkv, lane, p))
         return;
-    const tile_place tile(p, a.G, TILE_ROWS);
-    // (more pieces than slots: sequences whose rows overlap, of which the list of work is longer than the grid)
-    if (tile.pieces == 1 || p.slot + tile.pieces > slots)
+    const tile_place tile(p, a.G, part.rule.tile_rows);
+    const int64_t stride = part.rule.tile_rows * (D + 2);
+    // (more pieces than there is room for: sequences whose rows overlap, of which the list of work is longer than the grid)
+    if (tile.pieces == 1 || (p.slot + tile.pieces) * stride > room)
         return;
-    const int d = 2 * (lane % (D / 2)), first = (blockIdx.x * MERGE_WAVES + wave) * EACH;
-    for (int r = first; r < first + EACH && r < tile.rows; ++r) {
-        const float *from = partials + ((int64_t)h * slots + p.slot) * STRIDE + r * (D + 2);
+    const int d = 2 * (lane % (D / 2)), first = (group * MERGE_WAVES + wave) * part.each;
+    for (int r = first; r < first + part.each && r < tile.rows; ++r) {
+        const float *from = partials + h * room + p.slot * stride + r * (D + 2);
         float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
         constexpr int AT_ONCE = 16;  // loads on their way together
-        for (int c0 = 0; c0 < tile.pieces; c0 += AT_ONCE, from += (int64_t)AT_ONCE * STRIDE) {
+        for (int c0 = 0; c0 < tile.pieces; c0 += AT_ONCE, from += AT_ONCE * stride) {
             float2 ml[AT_ONCE], v[AT_ONCE];
 #pragma unroll
             for (int c = 0; c < AT_ONCE; ++c) {
-                const float *piece = from + (c0 + c < tile.pieces ? c : 0) * (int64_t)STRIDE;
+                const float *piece = from + (c0 + c < tile.pieces ? c : 0) * stride;
                 ml[c] = *(const float2 *)piece;
                 v[c] = *(const float2 *)(piece + 2 + d);
             }
@@ -308,58 +322,55 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_pag
     }
 }
 
-template <typename T, int D>
-void launch_merge(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int64_t few_tiles, int64_t tiles, hipStream_t s)
+merge_part part_of(const work_rule &rule, const float *partials, int64_t room, int64_t tiles, int each)
 {
-    constexpr int FEW_EACH = 1, TILE_EACH = 4;
-    if (w.few_budget > 0)
-        hipLaunchKernelGGL((pq_paged_merge_kernel<T, D, ROWS, FEW_EACH>), dim3(ROWS / (MERGE_WAVES * FEW_EACH), (unsigned)(few_tiles * a.c.Hkv)),
-                           dim3(64 * MERGE_WAVES), 0, s, a, few_rule(w), w.few_partials, w.few_slots);
-    if (w.tile_budget > 0)
-        hipLaunchKernelGGL((pq_paged_merge_kernel<T, D, PQ_PAGED_TILE_ROWS, TILE_EACH>),
-                           dim3(PQ_PAGED_TILE_ROWS / (MERGE_WAVES * TILE_EACH), (unsigned)(tiles * a.c.Hkv)), dim3(64 * MERGE_WAVES), 0, s, a,
-                           tile_rule(w), w.tile_partials, w.tile_slots);
+    return merge_part{rule, partials, room, rule.budget > 0 ? (int)tiles : 0, rule.tile_rows / (MERGE_WAVES * each), each};
 }
 
 }  // namespace
 
-// Pieces are as many as give every compute unit a workgroup of the kernel for many rows, or two of the one for few.
+// Pieces are as many as give every compute unit two workgroups.
+//
+// Where the line between the two kernels lies, measured with 32 query / 8 KV heads: 240 rows of one sequence over 8K keys 28 us
+// here, 39 as a tile of 256; 168 rows in each of 6 sequences over 1.6K keys (28 / 4 heads) 25 against 36; 180 rows in each of 4
+// over 8K keys 73 against 65.
 pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu)
 {
     pq_paged_prefill_plan w;
-    w.tile_budget = n_cu / cfg->n_kv_heads > 1 ? n_cu / cfg->n_kv_heads : 1;
-    w.few_budget = 2 * w.tile_budget;
-    w.tile_slots = 2 * w.tile_budget;
-    w.few_slots = 2 * w.few_budget;
+    const int per_head = n_cu / cfg->n_kv_heads > 1 ? n_cu / cfg->n_kv_heads : 1;
+    w.tile_budget = w.few_budget = 2 * per_head;
+    // entries of a call that is cut: the pieces that the budget allows and a rest for each tile, of which there are fewer than the
+    // budget
+    w.tile_room = 2 * (int64_t)w.tile_budget * (PQ_PAGED_TILE_ROWS / 2) * (cfg->head_dim + 2);
+    w.few_room = 2 * (int64_t)w.few_budget * PQ_PAGED_FEW_ROWS * (cfg->head_dim + 2);
     w.tile_partials = w.few_partials = nullptr;
-    // measured with 32 query / 8 KV heads over 8K keys: 180 rows in each of 4 sequences 73 us here, 65 us as tiles of 256; 240 rows
-    // of one sequence 28 against 39; 16 rows in each of 16 (4K keys) 41 against 67
-    w.few_rows = 128;
+    w.few_rows = 256;
+    w.tile_rows = PQ_PAGED_TILE_ROWS;
     return w;
-}
-
-int64_t pq_paged_prefill_partials(const pq_paged_config *cfg, const pq_paged_prefill_plan &w, bool few)
-{
-    return (int64_t)cfg->n_kv_heads * (few ? w.few_slots * PQ_PAGED_FEW_ROWS : w.tile_slots * PQ_PAGED_TILE_ROWS) * (cfg->head_dim + 2);
 }
 
 hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s)
 {
     pq_paged_prefill_plan w = ctx->prefill;
     const int64_t rows = (int64_t)a.n_tokens * a.G, seqs = a.n_seqs < a.n_tokens ? a.n_seqs : a.n_tokens;
-    // which kernels can have work: a single sequence is taken to have all rows
+    // Which kernels can have work: the one for few rows is left out where the sequences have many on average (four ragged prompts of
+    // up to 2000 tokens x 32 heads: 57 us, 62 with the launch that finds nothing).
     const bool many = rows > w.few_rows;
-    if (many && a.n_seqs == 1)
+    if (many && rows >= 2 * (int64_t)w.few_rows * a.n_seqs)
         w.few_rows = 0;
-    const int dtype = ctx->cfg.dtype, dim = ctx->cfg.head_dim;
-    // tiles there can be: every sequence's last may be a part of one.  A call that can have as many as the budget is not cut
-    // along the keys.
+    // Tiles there can be: every sequence's last may be a part of one.  Where whole tiles do not fill the chip they are halved (a
+    // prompt of 1000 tokens 48 us in whole ones, 35 in halves; where the keys are many whole ones would do more a step: 200
+    // tokens over 16K keys 88 against 104 us), and where halves are fewer than compute units they are cut along the keys as well
+    // (the same prompt, cut: 53 us).
     const int64_t few_most = seqs * ((w.few_rows + ROWS - 1) / ROWS), few_each = rows / ROWS + seqs;
-    const int64_t few_tiles = few_most < few_each ? few_most : few_each, tiles = rows / PQ_PAGED_TILE_ROWS + seqs;
+    const int64_t few_tiles = few_most < few_each ? few_most : few_each;
+    w.tile_rows = (rows / PQ_PAGED_TILE_ROWS + seqs) * a.c.Hkv < ctx->n_cu ? PQ_PAGED_TILE_ROWS / 2 : PQ_PAGED_TILE_ROWS;
+    const int64_t tiles = rows / w.tile_rows + seqs;
     if (few_tiles >= w.few_budget || w.few_rows == 0)
         w.few_budget = 0;
-    if (tiles >= w.tile_budget || !many)
+    if (2 * tiles >= w.tile_budget || w.tile_rows == PQ_PAGED_TILE_ROWS || !many)
         w.tile_budget = 0;
+    const int dtype = ctx->cfg.dtype, dim = ctx->cfg.head_dim;
     if (w.few_rows > 0) {
 #define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.few_budget) * a.c.Hkv)), dim3(THREADS), 0, s, a, w)
         PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
@@ -370,8 +381,13 @@ hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_
         if (e != hipSuccess)
             return e;
     }
-#define LAUNCH(T, D) launch_merge<T, D>(a, w, few_tiles, tiles, s)
-    PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
+    if (w.few_budget > 0 || w.tile_budget > 0) {
+        const merge_part few = part_of(few_rule(w), w.few_partials, w.few_room, few_tiles, 1);
+        const merge_part many = part_of(tile_rule(w), w.tile_partials, w.tile_room, tiles, 4);
+        const dim3 grid((unsigned)((few.tiles * few.groups + many.tiles * many.groups) * a.c.Hkv));
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_merge_kernel<T, D>), grid, dim3(64 * MERGE_WAVES), 0, s, a, few, many)
+        PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH
+    }
     return hipGetLastError();
 }

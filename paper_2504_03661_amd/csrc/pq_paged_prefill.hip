@@ -352,7 +352,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
     if (k0 < k1)
         values_32<S, PARTS>(rows, lds[before], PARTS_32 - 1, col, half, weights);
 
-    float *const part = w.tile_partials + ((int64_t)h * w.tile_slots + p.slot + p.split) * (TILE_ROWS * (D + 2));
+    float *const part = w.tile_partials + h * w.tile_room + (int64_t)(p.slot + p.split) * (TILE_ROWS * (D + 2));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float sum = rows.l[n] + __shfl_xor(rows.l[n], 32, 64);
@@ -389,13 +389,25 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
 
 }  // namespace
 
-// 64 keys of 128 dims, 128 of 64: 16 KiB of fp16 each of K and V
-template <int D> using shape_for = shape<D, 1, PQ_PAGED_TILE_ROWS / 32, 64 * 128 / D>;
+// Whole tiles: one workgroup a compute unit, 64 keys of 128 dims (128 of 64), 16 KiB of fp16 each of K and V.  Half tiles: two, with
+// half the keys.
+template <int D, int ROWS> using shape_for = shape<D, 1, ROWS / 32, ROWS / 4 * 128 / D>;
+
+template <typename T, int D, int ROWS> static void launch_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int64_t entries, hipStream_t s)
+{
+    using S = shape_for<D, ROWS>;
+    hipLaunchKernelGGL((pq_paged_prefill_kernel<T, S>), dim3((unsigned)(entries * a.c.Hkv)), dim3(S::THREADS), 0, s, a, w);
+}
 
 hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int dtype, int dim, int64_t entries, hipStream_t s)
 {
-#define LAUNCH(T, D)                                                                                                       \
-    hipLaunchKernelGGL((pq_paged_prefill_kernel<T, shape_for<D>>), dim3((unsigned)(entries * a.c.Hkv)), dim3(shape_for<D>::THREADS), 0, s, a, w)
+#define LAUNCH(T, D)                                                         \
+    do {                                                                     \
+        if (w.tile_rows == PQ_PAGED_TILE_ROWS)                               \
+            launch_tiles<T, D, PQ_PAGED_TILE_ROWS>(a, w, entries, s);        \
+        else                                                                 \
+            launch_tiles<T, D, PQ_PAGED_TILE_ROWS / 2>(a, w, entries, s);    \
+    } while (0)
     PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH
     return hipGetLastError();

@@ -39,7 +39,7 @@ __host__ __device__ inline work_rule few_rule(const pq_paged_prefill_plan &w)
 
 __host__ __device__ inline work_rule tile_rule(const pq_paged_prefill_plan &w)
 {
-    return work_rule{w.few_rows + 1, INT32_MAX, PQ_PAGED_TILE_ROWS, w.tile_budget};
+    return work_rule{w.few_rows + 1, INT32_MAX, w.tile_rows, w.tile_budget};
 }
 
 __device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule, int b, int &start, int &asked)
@@ -53,9 +53,9 @@ __device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule
 template <bool BY_TILE = false>
 __device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &rule, int e, int lane, work_place &p)
 {
-    const int tile_rows = rule.tile_rows, budget = rule.budget;
+    const int tile_rows = rule.tile_rows;
     p.keys = PQ_MAX_TOKENS;
-    if (budget > 0) {
+    if (rule.budget > 0) {
         float work = 0.0f;
         for (int b0 = 0; b0 < a.n_seqs; b0 += 64)
             if (b0 + lane < a.n_seqs) {
@@ -63,7 +63,7 @@ __device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &r
                 const int n = (rows_of(a, rule, b0 + lane, start, asked) * a.G + tile_rows - 1) / tile_rows;
                 work += (float)n * (float)paged_length(a.c, b0 + lane);
             }
-        p.keys = piece_tokens(wave_sum(work), budget, KEY_ALIGN, LEAST_KEYS);
+        p.keys = piece_tokens(wave_sum(work), rule.budget, KEY_ALIGN, LEAST_KEYS);
     }
     int before = 0, tiles_before = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
