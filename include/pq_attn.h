@@ -241,7 +241,8 @@ int pq_attn_device_error(pq_attn_ctx *ctx, uint32_t *flags /* host */);
  *
  * Blocks.  n_blocks blocks of block_tokens tokens.  Sequence b holds block_table[b][0 .. ceil(len / block_tokens) - 1];
  * its token at position p is in slot block_table[b][p / block_tokens] * block_tokens + p % block_tokens.  Requests may
- * name the same blocks (a shared prefix) as long as none of them appends to a shared one.
+ * name the same blocks (a shared prefix) as long as none of them appends to a shared one and the program keeps count of
+ * the holders: pq_paged_plan gives back all blocks of a request that ends.
  *
  * Values.  With x the values of one KV head's tokens in a block (K and V each for itself):
  *     scale = max(max |x|, 127 * 2^-40) / 127, rounded to fp32;  code = x / scale, rounded to the nearest integer, ties
@@ -348,7 +349,7 @@ int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_
  *   q                    as in pq_paged_decode, row t at t * q_stride elements
  *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
  *   tok_start, tok_len   device int32, as pq_paged_plan gives them (rows from n_tokens on are left out, a sequence whose
- *                        first row is outside [0, n_tokens) altogether)
+ *                        first row is outside [0, n_tokens) altogether; rows that two sequences claim hold nobody's result)
  *   out                  device [n_tokens][Hq][d] dtype; rows of no sequence are left as they were
  *
  * 0 <= n_tokens <= max_tokens; 0 does nothing. */

@@ -336,7 +336,7 @@ def pq_paged_destroy(ctx: int) -> None:
 
 
 def pq_paged_plan(ctx, n_seqs, n_tokens, n_new, seq_len, free_list, free_count, block_table, new_seq_len,
-                       new_free_count, tok_start, tok_len, slot_map, stream=None) -> None:
+                  new_free_count, tok_start, tok_len, slot_map, stream=None) -> None:
     L = _lib or load_library()
     if _calls is not None and isinstance(ctx, _CONTEXT):
         rc = _calls.paged_plan(_paged_at["plan"], _current_stream, ctx, n_seqs, n_tokens, n_new, seq_len, free_list,
@@ -351,7 +351,7 @@ def pq_paged_plan(ctx, n_seqs, n_tokens, n_new, seq_len, free_list, free_count, 
 
 
 def pq_paged_append(ctx, n_tokens, new_k, new_v, kv_stride, slot_map, k_cache, v_cache, k_scale, v_scale,
-                         stream=None) -> None:
+                    stream=None) -> None:
     L = _lib or load_library()
     if _calls is not None and isinstance(ctx, _CONTEXT):
         rc = _calls.paged_append(_paged_at["append"], _current_stream, ctx, n_tokens, new_k, new_v, kv_stride, slot_map,
@@ -364,7 +364,7 @@ def pq_paged_append(ctx, n_tokens, new_k, new_v, kv_stride, slot_map, k_cache, v
 
 
 def pq_paged_read(ctx, n_seqs, n_rows, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, first, out_k, out_v,
-                       stream=None) -> None:
+                  stream=None) -> None:
     L = _lib or load_library()
     if _calls is not None and isinstance(ctx, _CONTEXT):
         rc = _calls.paged_read(_paged_at["read"], _current_stream, ctx, n_seqs, n_rows, k_cache, v_cache, k_scale,
@@ -378,7 +378,7 @@ def pq_paged_read(ctx, n_seqs, n_rows, k_cache, v_cache, k_scale, v_scale, block
 
 
 def pq_paged_decode(ctx, n_seqs, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, scale, out,
-                         stream=None) -> None:
+                    stream=None) -> None:
     L = _lib or load_library()
     if _calls is not None and isinstance(ctx, _CONTEXT):
         rc = _calls.paged_decode(_paged_at["decode"], _current_stream, ctx, n_seqs, q, q_stride, k_cache, v_cache,
@@ -392,7 +392,7 @@ def pq_paged_decode(ctx, n_seqs, q, q_stride, k_cache, v_cache, k_scale, v_scale
 
 
 def pq_paged_prefill(ctx, n_seqs, n_tokens, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len,
-                          tok_start, tok_len, scale, out, stream=None) -> None:
+                     tok_start, tok_len, scale, out, stream=None) -> None:
     L = _lib or load_library()
     if _calls is not None and isinstance(ctx, _CONTEXT):
         rc = _calls.paged_prefill(_paged_at["prefill"], _current_stream, ctx, n_seqs, n_tokens, q, q_stride, k_cache,

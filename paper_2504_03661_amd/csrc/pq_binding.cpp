@@ -1,6 +1,6 @@
-// The per-step calls of the Python binding (pq_attn_decode, pq_encode_append, the five of the paged cache) without ctypes: arguments are taken apart
-// here, the library's functions are called through the addresses that binding.py hands over.  A decoding step of one
-// short sequence (32 heads, 1K tokens) is bound by the host: with ctypes the two calls took 13 us of the step, marshalling
+// The per-step calls of the Python binding (pq_attn_decode, pq_encode_append, the five of the paged cache) without ctypes:
+// arguments are taken apart here, the library's functions are called through the addresses that binding.py hands over.  A
+// decoding step of one short sequence (32 heads, 1K tokens) is bound by the host: with ctypes the two calls took 13 us of the step, marshalling
 // ten pointers each through Python helpers; with this module the step takes 16.1 us, before 22.8.
 //
 // As binding.py's helpers do it: a pointer argument is None (NULL), an int, or an object with data_ptr(); a stream is

@@ -179,8 +179,9 @@ def test_lengths_outside_the_table_are_clamped():
     assert (out[1] == 0).all()
 
 
-def prefill_case(rng, dtype, Hq, Hkv, dim, block, lengths, new, scale=0.1, gap=0, lead=0, tail=0):
-    """`lead` and `tail`: rows before the first and behind the last sequence's, that belong to nobody."""
+def prefill_case(rng, dtype, Hq, Hkv, dim, block, lengths, new, scale=0.1, gap=0, lead=0, tail=0, every=1):
+    """`lead` and `tail`: rows before the first and behind the last sequence's, that belong to nobody.  `every`: of a
+    sequence's rows the last and every such one before it are compared, the others are to be finite."""
     lengths, new = np.asarray(lengths), np.asarray(new)
     c = Filled(rng, lengths, Hkv, dim, block)
     start = lead + np.concatenate([[0], np.cumsum(new)])
@@ -191,10 +192,11 @@ def prefill_case(rng, dtype, Hq, Hkv, dim, block, lengths, new, scale=0.1, gap=0
     pq.pq_paged_prefill(ctx.handle, len(lengths), rows, q, q.shape[1], *c.args(), dev(start), dev(new), scale, out)
     assert (out[:lead] == 7.0).all() and (out[rows - tail:] == 7.0).all()
     for b in range(len(lengths)):
-        i = np.arange(new[b])
+        i = np.arange(new[b])[::-every][::-1]
         if len(i):
-            part = slice(int(start[b]), int(start[b]) + len(i))
+            part = int(start[b]) + i
             check(out[part], *c.attention(values[part], b, scale, lengths[b] - new[b] + i + 1), dtype, dim, f"sequence {b}")
+            assert out[int(start[b]):int(start[b]) + int(new[b])].isfinite().all()
     assert pq.pq_paged_device_error(ctx.handle) == 0
     return c, ctx, q, out, start
 
@@ -217,6 +219,22 @@ def test_prefill_lengths(dtype, dim, block, lengths, new):
 def test_prefill_of_few_rows_over_a_long_cache():
     for dtype in ("f16", "f32"):
         prefill_case(np.random.default_rng(20), dtype, 4, 1, 128, 16, [12000, 300, 5003], [5, 20, 33])
+
+
+LONG = [("f16", 128, 64), ("bf16", 128, 32), ("f32", 128, 16), ("f32", 128, 64), ("bf16", 64, 64), ("f16", 64, 16)]
+
+
+@pytest.mark.parametrize("dtype,dim,block", LONG)
+@pytest.mark.parametrize("heads,lengths,new", [
+    ((4, 2), [140, 130], [151, 3]),     # a tile that is cut along the keys, and few rows beside it
+    ((4, 1), [140], [300]),
+    ((64, 64), [75], [400]),            # half tiles, as many as fill a chip of 256 compute units uncut
+    ((128, 128), [70], [257]),          # whole tiles
+])
+def test_prefill_of_many_rows_over_a_long_cache(dtype, dim, block, heads, lengths, new):
+    """More than 256 rows of a KV head: tiles of keys that every wavefront of a workgroup uses, over more than one batch of 64
+    blocks (lengths in blocks)."""
+    prefill_case(np.random.default_rng(26), dtype, *heads, dim, block, [n * block - 9 for n in lengths], new, every=37)
 
 
 def test_prefill_of_one_token_is_decode():
