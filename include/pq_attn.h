@@ -266,7 +266,7 @@ typedef struct pq_paged_ctx pq_paged_ctx;
 typedef struct {
     int32_t max_seqs;     /* sequences of one call at most, 1 .. 4096                         */
     int32_t max_tokens;   /* new tokens of one call at most, over all sequences, 1 .. 2^20    */
-    int32_t n_q_heads;    /* Hq                                                              */
+    int32_t n_q_heads;    /* Hq, 1 .. 1024; max_tokens * Hq <= 2^28                          */
     int32_t n_kv_heads;   /* Hkv, Hq % Hkv == 0; query head h reads KV head h / (Hq / Hkv)    */
     int32_t head_dim;     /* d; supported: 64, 128                                           */
     int32_t block_tokens; /* supported: 16, 32, 64                                           */
@@ -323,7 +323,7 @@ int pq_paged_append(pq_paged_ctx *ctx, int32_t n_tokens, const void *new_k, cons
 
 /* Tokens of the cache in full precision: row r of sequence b is its token first[b] + r.
  *
- *   n_rows       rows per sequence, >= 0
+ *   n_rows       rows per sequence, 0 .. 2^24; n_seqs * Hkv * (n_rows + 8) * d <= 2^36, else PQ_ERR_CAPACITY
  *   first        device [n_seqs] int32, >= 0; NULL: all 0
  *   out_k/out_v  device [n_seqs][Hkv][n_rows][d] dtype, what pq_encode_append takes; rows behind a sequence's last
  *                token are left as they were */

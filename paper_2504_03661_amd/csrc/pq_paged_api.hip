@@ -30,6 +30,9 @@ int validate(const pq_paged_config *c)
     // slots are int32, positions and blocks of a sequence are worked out in 32 bits
     if ((int64_t)c->n_blocks * c->block_tokens > INT32_MAX || (int64_t)c->max_blocks * c->block_tokens > PQ_MAX_TOKENS)
         return PQ_ERR_UNSUPPORTED;
+    // launches have fewer than 2^32 threads: 8 for each row and head of it at most, and 2^31 for the sequences
+    if ((int64_t)c->max_tokens * c->n_q_heads > (int64_t)1 << 28)
+        return PQ_ERR_UNSUPPORTED;
     return PQ_OK;
 }
 
@@ -269,8 +272,8 @@ int pq_paged_read(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_rows, const uint8
         return rc;
     if (n_rows < 0 || !aligned(k_cache) || !aligned(v_cache) || !aligned(out_k) || !aligned(out_v))
         return PQ_ERR_SHAPE;
-    if (n_rows > PQ_MAX_TOKENS)
-        return PQ_ERR_CAPACITY;
+    if (n_rows > PQ_MAX_TOKENS || (int64_t)n_seqs * ctx->cfg.n_kv_heads * (n_rows + 8) * ctx->cfg.head_dim > (int64_t)1 << 36)
+        return PQ_ERR_CAPACITY;  // (a thread has 32 elements)
     if (n_rows == 0)
         return PQ_OK;
     device_guard guard(ctx->cfg.device);

@@ -237,6 +237,20 @@ def test_prefill_of_many_rows_over_a_long_cache(dtype, dim, block, heads, length
     prefill_case(np.random.default_rng(26), dtype, *heads, dim, block, [n * block - 9 for n in lengths], new, every=37)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("heads,seqs,longest", [
+    ((7, 1), 140, 900),                 # both kernels cut along the keys, half tiles
+    ((28, 4), 100, 700),                # neither cut, whole tiles
+])
+def test_prefill_of_many_ragged_sequences(dtype, heads, seqs, longest):
+    """More sequences than a wavefront looks at in one go, of which some bring many rows, most a few and some none."""
+    rng = np.random.default_rng(seqs)
+    lengths = rng.integers(0, longest, seqs)
+    lengths[[3, seqs - 2]] = 3 * longest
+    new = np.minimum(lengths, np.where(rng.random(seqs) < 0.2, rng.integers(20, 120, seqs), rng.integers(0, 5, seqs)))
+    prefill_case(rng, dtype, *heads, 64, 16, lengths, new, gap=8, lead=1, tail=2, every=11)
+
+
 def test_prefill_of_one_token_is_decode():
     rng = np.random.default_rng(21)
     lengths = [1, 40, 3001]

@@ -173,6 +173,30 @@ def test_append_of_a_long_prompt():
         store.check(str(block))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("dim,block", [(128, 16), (128, 32), (128, 64), (64, 16), (64, 32), (64, 64)])
+def test_append_of_a_ragged_batch_of_many_rows(dtype, dim, block):
+    """More rows times heads than get a unit each: several sequences' tokens lie in the rows that a unit looks through, their blocks
+    begin and end there, and older tokens stand in front of some."""
+    rng = np.random.default_rng(dim + block + 1)
+    seqs, Hkv, width = 44, 32, 6
+    store = Store(dtype, Hkv, dim, block, seqs * width)
+    table = rng.permutation(seqs * width).reshape(seqs, width)
+    length = np.zeros(seqs, int)
+    for step in range(2):
+        new = np.where(rng.random(seqs) < 0.4, rng.integers(1, 4, seqs), rng.integers(0, 2 * block + 10, seqs))
+        owner = np.repeat(np.arange(seqs), new)
+        assert len(owner) * 2 * Hkv > 64 * 256           # (256 compute units)
+        p = np.concatenate([np.arange(a, a + n) for a, n in zip(length, new)]).astype(int)
+        slots = table[owner, p // block] * block + p % block
+        slots[owner == 3 + step] = -1
+        store.append(draw(rng, len(slots), Hkv, dim), slots, gap=8)
+        length = length + new
+        length[3 + step] -= new[3 + step]
+        store.check(f"step {step}")
+    assert pq.pq_paged_device_error(store.ctx.handle) == 0
+
+
 def test_append_of_ties_small_numbers_and_what_is_not_finite():
     store = Store("f32", 6, 64, 16, 2)
     x = np.zeros((3, 6, 64), np.float32)

@@ -359,6 +359,17 @@ def test_refusals_launch_nothing():
     assert pq.pq_paged_device_error(h) == 0
 
 
+def test_read_refuses_more_than_a_launch_has_threads():
+    ctx = context("f16", 8, 8, 64, 16, 4, 2, 64)
+    length, table = dev([20] * 64), dev([[0, 1]] * 64)
+    data, scale = torch.zeros(4 * 8 * 16 * 64, dtype=torch.uint8, device="cuda"), torch.zeros((4, 8), device="cuda")
+    out = torch.full((16,), 3.0, dtype=torch.float16, device="cuda")
+    for rows in (2 ** 21 - 7, 2 ** 24):                                 # 64 x 8 x (rows + 8) x 64 against 2^36
+        refused(-4, pq.pq_paged_read, ctx.handle, 64, rows, data, data, scale, scale, table, length, None, out, out)
+    torch.cuda.synchronize()
+    assert (out == 3.0).all()
+
+
 def test_a_context_ends_with_its_object():
     c = context("f16", 2, 1, 64, 16, 4, 2, 1)
     assert c.handle

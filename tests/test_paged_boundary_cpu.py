@@ -40,6 +40,8 @@ def good(**kw):
     ({"max_seqs": 4097}, -3),
     ({"max_tokens": (1 << 20) + 1}, -3),
     ({"n_q_heads": 1032}, -3),
+    ({"n_q_heads": 1024, "max_tokens": 1 << 18}, 0),
+    ({"n_q_heads": 1024, "max_tokens": (1 << 18) + 1}, -3),     # more threads than a launch has
     ({"n_blocks": 1 << 27}, -3),                                # slots beyond 31 bits
     ({"n_blocks": (1 << 27) - 1}, 0),
     ({"max_blocks": (1 << 20) + 1}, -3),                        # sequences longer than 2^24 tokens
