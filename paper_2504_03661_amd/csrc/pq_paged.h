@@ -22,16 +22,13 @@ struct pq_paged_decode_plan {
 };
 
 // How pq_paged_prefill shares out a call: sequences of at most few_rows rows (tokens times query heads of a KV head) in tiles of
-// PQ_PAGED_FEW_ROWS, the others in tiles of tile_rows, PQ_PAGED_TILE_ROWS or half of them.  Budgets: pieces per KV head that a
-// call of few tiles is cut into along the keys; 0: not cut.  Partials: for each KV head *_room floats, [slot]
-// [rows of a tile][d + 2]: maximum, sum, sums of values.
+// PQ_PAGED_FEW_ROWS, whose keys are cut into about `budget` pieces per KV head (0: not cut), the others in tiles of
+// PQ_PAGED_TILE_ROWS.  Partials: for each KV head [2 budget slots][PQ_PAGED_FEW_ROWS][d + 2]: maximum, sum, sums of values.
 #define PQ_PAGED_TILE_ROWS 256
 #define PQ_PAGED_FEW_ROWS 32
 struct pq_paged_prefill_plan {
-    float *tile_partials, *few_partials;
-    int64_t tile_room, few_room;
-    int tile_budget, few_budget;
-    int few_rows, tile_rows;
+    float *partials;
+    int budget, few_rows;
 };
 
 struct pq_paged_ctx {
@@ -101,6 +98,7 @@ int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_
 int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
 hipError_t pq_launch_paged_decode(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu);
+int64_t pq_paged_prefill_floats(const pq_paged_config *cfg, const pq_paged_prefill_plan &w);
 hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int dtype, int dim, int64_t entries, hipStream_t s);
 hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s);
 

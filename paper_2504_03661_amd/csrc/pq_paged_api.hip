@@ -154,8 +154,7 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     const size_t zeros = bytes;
     const size_t plan_at = room((size_t)pq_paged_plan_scratch_bytes());
     const size_t decode_at = room((size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float));
-    const size_t tile_at = room((size_t)cfg->n_kv_heads * ctx->prefill.tile_room * sizeof(float));
-    const size_t few_at = room((size_t)cfg->n_kv_heads * ctx->prefill.few_room * sizeof(float));
+    const size_t prefill_at = room((size_t)pq_paged_prefill_floats(cfg, ctx->prefill) * sizeof(float));
     if (hipMalloc((void **)&ctx->scratch, bytes) != hipSuccess) {
         (void)hipGetLastError();
         delete ctx;
@@ -165,8 +164,7 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     ctx->decode.tickets = (unsigned int *)(ctx->scratch + tickets_at);
     ctx->plan = (int *)(ctx->scratch + plan_at);
     ctx->decode.partials = (float *)(ctx->scratch + decode_at);
-    ctx->prefill.tile_partials = (float *)(ctx->scratch + tile_at);
-    ctx->prefill.few_partials = (float *)(ctx->scratch + few_at);
+    ctx->prefill.partials = (float *)(ctx->scratch + prefill_at);
     if (hipMemset(ctx->scratch, 0, zeros) != hipSuccess || hipDeviceSynchronize() != hipSuccess) {
         (void)hipGetLastError();
         free_ctx(ctx);

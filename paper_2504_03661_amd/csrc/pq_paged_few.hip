@@ -1,12 +1,13 @@
-// pq_paged_prefill's other kernel, for sequences that bring few tokens: chunks, guessed tokens, the odd step among prompts.
-// And what both of them share: the merge of pieces, and the launches.
+// pq_paged_prefill's other kernel, for sequences that bring few tokens — chunks, guessed tokens, the odd step among prompts — and
+// for calls that are small as a whole.  And the merge of its pieces, and the launches.
 //
 // A workgroup has 32 rows (a token's query heads of a KV head side by side) and a piece of the keys that they see, of which each
 // of its four wavefronts takes a part, as pq_paged_decode's do: bytes go from memory to the lanes that multiply them, with
 // no LDS between.  The products are those of the kernel for many rows, 32x32x16, with K's dims in the order that 16-byte loads
 // bring them and V's dims in that of its 16-byte words.
 //
-// Bound by HBM where a sequence has one or two tiles, then by the conversion of bytes, which every tile does for itself.
+// Bound by latency and the merge where the work is small (12 tokens, 32 query / 8 KV heads, over 20K keys: 24 us for 41 MB), then by
+// the conversion of bytes, which every tile of 32 rows does for itself: 1000 tokens over 8K keys 195 us, 663 TFLOP/s.
 #include <hip/hip_runtime.h>
 
 #include "pq_paged_work.h"
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
         row_l[r] = sum;
     }
     __syncthreads();
-    float *const to = w.few_partials + h * w.few_room + (int64_t)(p.slot + p.split) * (ROWS * (D + 2));
+    float *const to = w.partials + ((int64_t)h * (2 * w.budget) + p.slot + p.split) * (ROWS * (D + 2));
     for (int i = threadIdx.x; i < tile.rows * (D / 2); i += THREADS) {
         const int r = i / (D / 2), d = i % (D / 2) * 2;
         float x = 0.0f, y = 0.0f;
@@ -259,57 +260,46 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     }
 }
 
-// The merge of both kernels' tiles in one launch: tiles are [few, whole or half], a workgroup has MERGE_WAVES times `each` rows.
-struct merge_part {
-    work_rule rule;
-    const float *partials;
-    int64_t room;
-    int tiles, groups, each;  // tiles that there can be, workgroups of a tile
-};
+constexpr int MERGE_WAVES = 4, MERGE_GROUPS = ROWS / MERGE_WAVES;  // workgroups of a tile, a wavefront has one row
 
-constexpr int MERGE_WAVES = 4;
-
-// Puts the pieces of a tile's keys together, a wavefront for some rows, one after another, and two dims a lane.
+// Puts the pieces of a tile's keys together, two dims a lane.
 template <typename T, int D>
-__global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_paged_attn_args a, merge_part few, merge_part many)
+__global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_paged_attn_args a, pq_paged_prefill_plan w)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int few_groups = few.tiles * few.groups * a.c.Hkv;
-    const bool is_few = (int)blockIdx.x < few_groups;
-    const int at = is_few ? blockIdx.x : blockIdx.x - few_groups;
-    const merge_part &part = is_few ? few : many;
-    const int group = at % part.groups, h = at / part.groups % a.c.Hkv;
-    const float *const partials = part.partials;
-    const int64_t room = part.room;
+    const int group = blockIdx.x % MERGE_GROUPS, h = blockIdx.x / MERGE_GROUPS % a.c.Hkv;
     work_place p;
-    if (!find_work<true>(a, part.rule, at / part.groups / a.c.Hkv, lane, p))
+    if (!find_work<true>(a, few_rule(w), blockIdx.x / MERGE_GROUPS / a.c.Hkv, lane, p))
         return;
-    const tile_place tile(p, a.G, part.rule.tile_rows);
-    const int64_t stride = part.rule.tile_rows * (D + 2);
-    // (more pieces than there is room for: sequences whose rows overlap, of which the list of work is longer than the grid)
-    if (tile.pieces == 1 || (p.slot + tile.pieces) * stride > room)
+    const tile_place tile(p, a.G, ROWS);
+    constexpr int64_t stride = ROWS * (D + 2);
+    if (tile.pieces == 1)
         return;
-    const int d = 2 * (lane % (D / 2)), first = (group * MERGE_WAVES + wave) * part.each;
-    for (int r = first; r < first + part.each && r < tile.rows; ++r) {
-        const float *from = partials + h * room + p.slot * stride + r * (D + 2);
+    const int d = 2 * (lane % (D / 2)), r = group * MERGE_WAVES + wave;
+    if (r < tile.rows) {
+        const float *from = w.partials + ((int64_t)h * (2 * w.budget) + p.slot) * stride + r * (D + 2);
         float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
-        constexpr int AT_ONCE = 16;  // loads on their way together
-        for (int c0 = 0; c0 < tile.pieces; c0 += AT_ONCE, from += AT_ONCE * stride) {
-            float2 ml[AT_ONCE], v[AT_ONCE];
+        for (int c0 = 0; c0 < tile.pieces; c0 += 64, from += 64 * stride) {
+            // a lane has a piece's maximum and sum, and so its weight; one that is not there has the weight 0
+            const int n = tile.pieces - c0 < 64 ? tile.pieces - c0 : 64;
+            const float2 ml = lane < n ? *(const float2 *)(from + lane * stride) : make_float2(-INFINITY, 0.0f);
+            const float high = fmaxf(top, wave_max(ml.x)), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
+            top = high;
+            sum = fmaf(sum, old, wave_sum(ml.y * by));
+            x *= old;
+            y *= old;
+            constexpr int AT_ONCE = 16;  // loads on their way together
+            for (int c1 = 0; c1 < n; c1 += AT_ONCE) {
+                float2 v[AT_ONCE];
 #pragma unroll
-            for (int c = 0; c < AT_ONCE; ++c) {
-                const float *piece = from + (c0 + c < tile.pieces ? c : 0) * stride;
-                ml[c] = *(const float2 *)piece;
-                v[c] = *(const float2 *)(piece + 2 + d);
-            }
+                for (int c = 0; c < AT_ONCE; ++c)
+                    v[c] = *(const float2 *)(from + (c1 + c < n ? c1 + c : 0) * stride + 2 + d);
 #pragma unroll
-            for (int c = 0; c < AT_ONCE; ++c) {
-                const float m = c0 + c < tile.pieces ? ml[c].x : -INFINITY;  // (a repeated one counts for nothing)
-                const float high = fmaxf(top, m), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(m - high);
-                top = high;
-                sum = fmaf(ml[c].y, by, sum * old);
-                x = fmaf(v[c].x, by, x * old);
-                y = fmaf(v[c].y, by, y * old);
+                for (int c = 0; c < AT_ONCE; ++c) {
+                    const float weight = lane_of(by, c1 + c);
+                    x = fmaf(v[c].x, weight, x);
+                    y = fmaf(v[c].y, weight, y);
+                }
             }
         }
         if (lane < D / 2) {
@@ -322,70 +312,56 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_pag
     }
 }
 
-merge_part part_of(const work_rule &rule, const float *partials, int64_t room, int64_t tiles, int each)
-{
-    return merge_part{rule, partials, room, rule.budget > 0 ? (int)tiles : 0, rule.tile_rows / (MERGE_WAVES * each), each};
-}
-
 }  // namespace
 
 // Pieces are as many as give every compute unit two workgroups.
-//
-// Where the line between the two kernels lies, measured with 32 query / 8 KV heads: 240 rows of one sequence over 8K keys 28 us
-// here, 39 as a tile of 256; 168 rows in each of 6 sequences over 1.6K keys (28 / 4 heads) 25 against 36; 180 rows in each of 4
-// over 8K keys 73 against 65.
 pq_paged_prefill_plan pq_paged_plan_prefill(const pq_paged_config *cfg, int n_cu)
 {
     pq_paged_prefill_plan w;
-    const int per_head = n_cu / cfg->n_kv_heads > 1 ? n_cu / cfg->n_kv_heads : 1;
-    w.tile_budget = w.few_budget = 2 * per_head;
-    // entries of a call that is cut: the pieces that the budget allows and a rest for each tile, of which there are fewer than the
-    // budget
-    w.tile_room = 2 * (int64_t)w.tile_budget * (PQ_PAGED_TILE_ROWS / 2) * (cfg->head_dim + 2);
-    w.few_room = 2 * (int64_t)w.few_budget * PQ_PAGED_FEW_ROWS * (cfg->head_dim + 2);
-    w.tile_partials = w.few_partials = nullptr;
+    w.budget = 2 * (n_cu / cfg->n_kv_heads > 1 ? n_cu / cfg->n_kv_heads : 1);
     w.few_rows = 256;
-    w.tile_rows = PQ_PAGED_TILE_ROWS;
+    w.partials = nullptr;
     return w;
+}
+
+int64_t pq_paged_prefill_floats(const pq_paged_config *cfg, const pq_paged_prefill_plan &w)
+{
+    return (int64_t)cfg->n_kv_heads * (2 * w.budget) * PQ_PAGED_FEW_ROWS * (cfg->head_dim + 2);
 }
 
 hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_args &a, hipStream_t s)
 {
     pq_paged_prefill_plan w = ctx->prefill;
     const int64_t rows = (int64_t)a.n_tokens * a.G, seqs = a.n_seqs < a.n_tokens ? a.n_seqs : a.n_tokens;
-    // Which kernels can have work: the one for few rows is left out where the sequences have many on average (four ragged prompts of
-    // up to 2000 tokens x 32 heads: 57 us, 62 with the launch that finds nothing).
-    const bool many = rows > w.few_rows;
-    if (many && rows >= 2 * (int64_t)w.few_rows * a.n_seqs)
+    // Which kernels can have work.  The one for few rows has all of it where the other's tiles would not fill three quarters of the
+    // chip (32 query / 8 KV heads over 8K keys: 1000 tokens 195 us here and 262 in tiles of 256 rows, 1500 tokens 277 and 277, 2000
+    // tokens 359 and 278), and none where sequences have many rows on average (four ragged prompts of up to 2000 tokens x 32 heads:
+    // 57 us, 62 with the launch that finds nothing).
+    if (4 * rows * a.c.Hkv < 3 * (int64_t)PQ_PAGED_TILE_ROWS * ctx->n_cu)
+        w.few_rows = INT32_MAX - 1;
+    else if (rows >= 2 * (int64_t)w.few_rows * a.n_seqs)
         w.few_rows = 0;
-    // Tiles there can be: every sequence's last may be a part of one.  Where whole tiles do not fill the chip they are halved (a
-    // prompt of 1000 tokens 48 us in whole ones, 35 in halves; where the keys are many whole ones would do more a step: 200
-    // tokens over 16K keys 88 against 104 us), and where halves are fewer than compute units they are cut along the keys as well
-    // (the same prompt, cut: 53 us).
-    const int64_t few_most = seqs * ((w.few_rows + ROWS - 1) / ROWS), few_each = rows / ROWS + seqs;
-    const int64_t few_tiles = few_most < few_each ? few_most : few_each;
-    w.tile_rows = (rows / PQ_PAGED_TILE_ROWS + seqs) * a.c.Hkv < ctx->n_cu ? PQ_PAGED_TILE_ROWS / 2 : PQ_PAGED_TILE_ROWS;
-    const int64_t tiles = rows / w.tile_rows + seqs;
-    if (few_tiles >= w.few_budget || w.few_rows == 0)
-        w.few_budget = 0;
-    if (2 * tiles >= w.tile_budget || w.tile_rows == PQ_PAGED_TILE_ROWS || !many)
-        w.tile_budget = 0;
+    // tiles there can be: every sequence's last may be a part of one
+    const int64_t each = rows / ROWS + seqs, most = seqs * ((w.few_rows + (int64_t)ROWS - 1) / ROWS), few_tiles = each < most ? each : most;
+    // No tile is cut if no sequence can be long enough, nor one sequence's tiles, which are alike, where every compute unit has one
+    // (250 tokens over 2000 keys 21 us, cut 34, over 10000 keys 78 and 85).
+    if ((ctx->cfg.max_blocks << ctx->log_block) <= WHOLE_KEYS || (a.n_seqs == 1 && 2 * few_tiles >= w.budget))
+        w.budget = 0;
     const int dtype = ctx->cfg.dtype, dim = ctx->cfg.head_dim;
     if (w.few_rows > 0) {
-#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.few_budget) * a.c.Hkv)), dim3(THREADS), 0, s, a, w)
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.budget) * a.c.Hkv)), dim3(THREADS), 0, s, a, w)
         PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH
     }
-    if (many) {
-        const hipError_t e = pq_launch_paged_tiles(a, w, dtype, dim, tiles + w.tile_budget, s);
+    if (rows > w.few_rows) {
+        const hipError_t e = pq_launch_paged_tiles(a, w, dtype, dim, rows / PQ_PAGED_TILE_ROWS + seqs, s);
         if (e != hipSuccess)
             return e;
     }
-    if (w.few_budget > 0 || w.tile_budget > 0) {
-        const merge_part few = part_of(few_rule(w), w.few_partials, w.few_room, few_tiles, 1);
-        const merge_part many = part_of(tile_rule(w), w.tile_partials, w.tile_room, tiles, 4);
-        const dim3 grid((unsigned)((few.tiles * few.groups + many.tiles * many.groups) * a.c.Hkv));
-#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_merge_kernel<T, D>), grid, dim3(64 * MERGE_WAVES), 0, s, a, few, many)
+    if (w.few_rows > 0 && w.budget > 0) {
+        const int64_t cut = few_tiles < w.budget ? few_tiles : w.budget;  // tiles that can have several pieces, of 2 budget in all
+        const dim3 grid((unsigned)(cut * MERGE_GROUPS * a.c.Hkv));
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_merge_kernel<T, D>), grid, dim3(64 * MERGE_WAVES), 0, s, a, w)
         PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH
     }

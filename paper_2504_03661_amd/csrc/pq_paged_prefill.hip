@@ -7,10 +7,8 @@
 // scores came in (V's tokens lie in LDS in the order in which the result of the first product holds them).  A lane has one query
 // row: its maximum, sum, limit and rescaling are its own.
 //
-// Few tiles over many keys: the keys of a tile are cut into pieces as well, which a kernel of their own puts together.
-//
 // Bound by the issue of matrix and vector instructions, which two wavefronts of a SIMD overlap only in part: a prompt of 8K tokens,
-// 32 query / 8 KV heads of 128 dims in bf16, takes 588 us (935 TFLOP/s; matrix units busy 36 % of the time, vector units 57 %).
+// 32 query / 8 KV heads of 128 dims in bf16, takes 594 us (925 TFLOP/s; matrix units busy 36 % of the time, vector units 57 %).
 // Without its exponentials it would take 20 us less, without the conversion of bytes 61, without the search for the maximum
 // 50, without the second product 156: no one of them stands out.
 #include <hip/hip_runtime.h>
@@ -26,7 +24,7 @@ template <int D_, int NT_, int WAVES_, int KEYS_> struct shape {
     static constexpr int D = D_, NT = NT_, WAVES = WAVES_, KEYS = KEYS_, THREADS = 64 * WAVES, ROWS = 32 * NT * WAVES;
     static constexpr int LOADS = KEYS * D / (THREADS * 16);  // 16-byte loads a thread makes of K, and of V
     static constexpr int K_PLANE = KEYS * 16 + 16;           // bytes of 8 dims of all keys, and a shift of 4 banks
-    static_assert(LOADS >= 1 && KEYS * D % (THREADS * 16) == 0 && KEYS % 32 == 0 && KEYS <= 128);
+    static_assert(LOADS >= 1 && KEYS * D % (THREADS * 16) == 0 && (KEYS == 64 || KEYS == 128));
 };
 
 template <typename S> struct tile_lds {
@@ -228,7 +226,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
 {
     constexpr bool SPLIT = sizeof(T) == 4;  // two fp16 parts of queries and weights
     constexpr int PARTS = SPLIT ? 2 : 1, D = S::D, NT = S::NT, DT = D / 32, TILE_ROWS = S::ROWS, KEYS = S::KEYS;
-    constexpr int BUFFERS = S::KEYS / 32 > 1 ? 3 : 4;
+    constexpr int BUFFERS = 3;
     __shared__ tile_lds<S> lds[BUFFERS];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -238,10 +236,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
         return;
     const int col = lane & 31, half = lane >> 5;
     const tile_place tile(p, a.G, TILE_ROWS);
-    const int past = p.past, row0 = tile.row0, all_rows = row0 + tile.rows, pieces = tile.pieces;
-    if (p.split >= pieces)
-        return;
-    const int k0 = p.split * p.keys, k1 = k0 + p.keys < tile.sees ? k0 + p.keys : tile.sees;
+    const int past = p.past, row0 = tile.row0, all_rows = row0 + tile.rows, k1 = tile.sees;
 
     // this lane's rows
     row_state<S, PARTS> rows;
@@ -292,7 +287,7 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
     wave_sees = __builtin_amdgcn_readfirstlane(wave_sees < k1 ? wave_sees : k1);
 
     const int32_t *table = a.c.table + (int64_t)p.b * a.c.max_blocks;
-    const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block, per_tile = (KEYS + (1 << a.c.log_block) - 1) >> a.c.log_block;
+    const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block, per_tile = KEYS >> a.c.log_block;
     // Three tiles in LDS: the one whose keys are scored, the one whose values were not all used yet, the one that is filled.
     // A tile is stored after the barrier behind which nobody reads the tile it takes the place of, and read after the next.
     constexpr int PARTS_32 = KEYS / 32;
@@ -313,12 +308,12 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
             batch = load_batch(a.c, table, j, last_block, h, lane);
         load_keys<S>(a.c, batch, h, t, wave, lane, bytes);
     };
-    if (k0 < k1) {
+    if (k1 > 0) {
         batch.first = -65;
-        load(k0);
-        store_keys<S>(lds[0], batch, a.c.log_block, k0, wave, lane, bytes);
-        if (k0 + KEYS < k1)
-            load(k0 + KEYS);
+        load(0);
+        store_keys<S>(lds[0], batch, a.c.log_block, 0, wave, lane, bytes);
+        if (KEYS < k1)
+            load(KEYS);
         __syncthreads();
         dots_32<S, PARTS>(rows, lds[0], 0, col, half, dot);
     }
@@ -330,8 +325,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
     asm volatile("" : "+v"(last));
     int at = 0, before = 0;  // the tile's place in LDS, and that of the tile in front of it
     // one step behind the last that the wavefront's rows see: it adds that one's values, and its own weights are all 0
-    const int wave_end = wave_sees > k0 ? k0 + (wave_sees - k0 + 31) / 32 * 32 + 32 : k0;
-    for (int t = k0; t < last; t += KEYS) {
+    const int wave_end = wave_sees > 0 ? (wave_sees + 31) / 32 * 32 + 32 : 0;
+    for (int t = 0; t < last; t += KEYS) {
         const int next = at == BUFFERS - 1 ? 0 : at + 1;
 #pragma unroll
         for (int u = 0; u < PARTS_32; ++u) {
@@ -352,64 +347,38 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
         before = at;
         at = next;
     }
-    if (k0 < k1)
+    if (k1 > 0)
         values_32<S, PARTS>(rows, lds[before], PARTS_32 - 1, col, half, weights);
 
-    float *const part = w.tile_partials + h * w.tile_room + (int64_t)(p.slot + p.split) * (TILE_ROWS * (D + 2));
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const float sum = rows.l[n] + __shfl_xor(rows.l[n], 32, 64);
-        const int r = (wave * NT + n) * 32 + col;
         if (token[n] < 0)
             continue;
-        if (pieces == 1) {
-            const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-            T *out = (T *)a.out + ((int64_t)(p.first_row + token[n]) * a.Hq + h * a.G + head[n]) * D + 4 * half;
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        T *out = (T *)a.out + ((int64_t)(p.first_row + token[n]) * a.Hq + h * a.G + head[n]) * D + 4 * half;
 #pragma unroll
-            for (int i = 0; i < DT; ++i)
+        for (int i = 0; i < DT; ++i)
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) {
-                    T x[4];
+            for (int j = 0; j < 16; j += 4) {
+                T x[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        x[e] = paged_elem<T>::down(rows.o[i][n][j + e] * by);
-                    __builtin_memcpy(out + 32 * i + 2 * j, x, sizeof(x));
-                }
-        } else {
-            float *to = part + r * (D + 2);
-            if (half == 0) {
-                to[0] = rows.m[n];
-                to[1] = sum;
+                for (int e = 0; e < 4; ++e)
+                    x[e] = paged_elem<T>::down(rows.o[i][n][j + e] * by);
+                __builtin_memcpy(out + 32 * i + 2 * j, x, sizeof(x));
             }
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; j += 2)
-                    *(float2 *)(to + 2 + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3)) = make_float2(rows.o[i][n][j], rows.o[i][n][j + 1]);
-        }
     }
 }
 
 }  // namespace
 
-// Whole tiles: one workgroup a compute unit, 64 keys of 128 dims (128 of 64), 16 KiB of fp16 each of K and V.  Half tiles: two, with
-// half the keys.
-template <int D, int ROWS> using shape_for = shape<D, 1, ROWS / 32, ROWS / 4 * 128 / D>;
-
-template <typename T, int D, int ROWS> static void launch_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int64_t entries, hipStream_t s)
+// Tiles of 256 rows, one workgroup a compute unit; 64 keys of 128 dims (128 of 64), 16 KiB of fp16 each of K and V.
+hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int dtype, int dim, int64_t tiles, hipStream_t s)
 {
-    using S = shape_for<D, ROWS>;
-    hipLaunchKernelGGL((pq_paged_prefill_kernel<T, S>), dim3((unsigned)(entries * a.c.Hkv)), dim3(S::THREADS), 0, s, a, w);
-}
-
-hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_prefill_plan &w, int dtype, int dim, int64_t entries, hipStream_t s)
-{
-#define LAUNCH(T, D)                                                         \
-    do {                                                                     \
-        if (w.tile_rows == PQ_PAGED_TILE_ROWS)                               \
-            launch_tiles<T, D, PQ_PAGED_TILE_ROWS>(a, w, entries, s);        \
-        else                                                                 \
-            launch_tiles<T, D, PQ_PAGED_TILE_ROWS / 2>(a, w, entries, s);    \
+#define LAUNCH(T, D)                                                                                                          \
+    do {                                                                                                                      \
+        using S = shape<D, 1, PQ_PAGED_TILE_ROWS / 32, 64 * 128 / D>;                                                         \
+        hipLaunchKernelGGL((pq_paged_prefill_kernel<T, S>), dim3((unsigned)(tiles * a.c.Hkv)), dim3(S::THREADS), 0, s, a, w); \
     } while (0)
     PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH

@@ -6,13 +6,16 @@
 
 namespace {
 
-constexpr int KEY_ALIGN = 128, LEAST_KEYS = 512;  // of a piece of a tile's keys
+// A piece of a tile's keys: a multiple of KEY_ALIGN, LEAST_KEYS at least.  Tiles of up to WHOLE_KEYS keys are not cut, where there
+// are tiles for half of the compute units twice as many: pieces cost more than they save then (32 query / 8 KV heads, 187 tokens
+// over 2000 keys: 24 us whole, 33 cut; four times 100 tokens over 2000: 38 and 51; but 12 tokens over 2000: 21 and 15).
+constexpr int KEY_ALIGN = 128, LEAST_KEYS = 512, WHOLE_KEYS = 1024;
 
 struct work_place {
     int b, len, first_row, rows;  // sequence, its length, its first row of the tensors, its rows there
     int past;                     // keys in front of its first row's own (negative: the first rows see nothing)
     int tile, split, keys;        // tile of its rows, piece of the keys, keys of a piece
-    int slot;                     // of the tile's first piece among the call's
+    int slot;                     // of the tile's first piece among the pieces of tiles that are cut
 };
 
 // Rows of sequence b that lie in the tensors
@@ -32,15 +35,8 @@ struct work_rule {
     int budget;       // pieces that the keys of all tiles together are cut into at most, and a rest for each tile; 0: one a tile
 };
 
-__host__ __device__ inline work_rule few_rule(const pq_paged_prefill_plan &w)
-{
-    return work_rule{1, w.few_rows, PQ_PAGED_FEW_ROWS, w.few_budget};
-}
-
-__host__ __device__ inline work_rule tile_rule(const pq_paged_prefill_plan &w)
-{
-    return work_rule{w.few_rows + 1, INT32_MAX, w.tile_rows, w.tile_budget};
-}
+__device__ inline work_rule few_rule(const pq_paged_prefill_plan &w) { return work_rule{1, w.few_rows, PQ_PAGED_FEW_ROWS, w.budget}; }
+__device__ inline work_rule tile_rule(const pq_paged_prefill_plan &w) { return work_rule{w.few_rows + 1, INT32_MAX, PQ_PAGED_TILE_ROWS, 0}; }
 
 __device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule, int b, int &start, int &asked)
 {
@@ -49,34 +45,42 @@ __device__ inline int rows_of(const pq_paged_attn_args &a, const work_rule &rule
 }
 
 // Entry e of the list of a kernel's work: sequence after sequence, tile after tile (those that see most first), the pieces of a
-// tile's keys.  BY_TILE: tile e instead, its first piece.
-template <bool BY_TILE = false>
+// tile's keys.  All sequences are cut into pieces about as long as each other, each into equal ones.  That makes at most
+// `budget` pieces and a rest for each tile, and those of tiles that have several are at most 2 `budget`.
+// CUT_ONLY: e counts the tiles that have several pieces instead, and its first piece is given.
+template <bool CUT_ONLY = false>
 __device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &rule, int e, int lane, work_place &p)
 {
     const int tile_rows = rule.tile_rows;
-    p.keys = PQ_MAX_TOKENS;
+    int most_keys = PQ_MAX_TOKENS, whole_keys = PQ_MAX_TOKENS;
     if (rule.budget > 0) {
-        float work = 0.0f;
+        float work = 0.0f, of_tiles = 0.0f;
         for (int b0 = 0; b0 < a.n_seqs; b0 += 64)
             if (b0 + lane < a.n_seqs) {
                 int start, asked;
                 const int n = (rows_of(a, rule, b0 + lane, start, asked) * a.G + tile_rows - 1) / tile_rows;
+                of_tiles += (float)n;
                 work += (float)n * (float)paged_length(a.c, b0 + lane);
             }
-        p.keys = piece_tokens(wave_sum(work), rule.budget, KEY_ALIGN, LEAST_KEYS);
+        most_keys = piece_tokens(wave_sum(work), rule.budget, KEY_ALIGN, LEAST_KEYS);
+        whole_keys = 4.0f * wave_sum(of_tiles) < (float)rule.budget ? WHOLE_KEYS : 2 * WHOLE_KEYS;
     }
-    int before = 0, tiles_before = 0;
+    int before = 0, slots = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 64) {
-        int start = 0, asked = 0, rows = 0, len = 0, per_tile = 1, tiles = 0;
+        int start = 0, asked = 0, rows = 0, len = 0, keys = PQ_MAX_TOKENS, per_tile = 1, tiles = 0;
         if (b0 + lane < a.n_seqs) {
             rows = rows_of(a, rule, b0 + lane, start, asked);
             len = paged_length(a.c, b0 + lane);
-            per_tile = len > 0 ? (len + p.keys - 1) / p.keys : 1;
             tiles = (rows * a.G + tile_rows - 1) / tile_rows;
+            if (len > most_keys && len > whole_keys) {
+                const int n = (len + most_keys - 1) / most_keys;
+                keys = ((len + n - 1) / n + KEY_ALIGN - 1) / KEY_ALIGN * KEY_ALIGN;
+                per_tile = (len + keys - 1) / keys;
+            }
         }
-        const int n = tiles * per_tile, upto = before + lane_scan(n), tiles_upto = BY_TILE ? tiles_before + lane_scan(tiles) : 0;
-        const bool mine = BY_TILE ? e >= tiles_upto - tiles && e < tiles_upto : e >= upto - n && e < upto;
-        const uint64_t found = __ballot(mine);
+        const int n = CUT_ONLY && per_tile == 1 ? 0 : CUT_ONLY ? tiles : tiles * per_tile, upto = before + lane_scan(n);
+        const int several = per_tile > 1 ? tiles * per_tile : 0, slot = slots + lane_scan(several) - several;
+        const uint64_t found = __ballot(e >= upto - n && e < upto);
         if (found != 0) {
             const int l = __builtin_ctzll(found);
             p.b = b0 + l;
@@ -84,16 +88,16 @@ __device__ inline bool find_work(const pq_paged_attn_args &a, const work_rule &r
             p.first_row = __builtin_amdgcn_readlane(start, l);
             p.rows = __builtin_amdgcn_readlane(rows, l);
             p.past = p.len - __builtin_amdgcn_readlane(asked, l);
+            p.keys = __builtin_amdgcn_readlane(keys, l);
             const int each = __builtin_amdgcn_readlane(per_tile, l), all = __builtin_amdgcn_readlane(tiles, l);
-            const int first = __builtin_amdgcn_readlane(upto - n, l);
-            const int from_end = BY_TILE ? e - __builtin_amdgcn_readlane(tiles_upto - tiles, l) : (e - first) / each;
+            const int at = e - __builtin_amdgcn_readlane(upto - n, l), from_end = CUT_ONLY ? at : at / each;
             p.tile = all - 1 - from_end;
-            p.split = BY_TILE ? 0 : e - first - from_end * each;
-            p.slot = first + from_end * each;
+            p.split = CUT_ONLY ? 0 : at - from_end * each;
+            p.slot = __builtin_amdgcn_readlane(slot, l) + from_end * each;
             return true;
         }
         before = __builtin_amdgcn_readlane(upto, 63);
-        tiles_before = __builtin_amdgcn_readlane(tiles_upto, 63);
+        slots = __builtin_amdgcn_readlane(slot + several, 63);
     }
     return false;
 }

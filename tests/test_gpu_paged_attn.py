@@ -226,21 +226,25 @@ LONG = [("f16", 128, 64), ("bf16", 128, 32), ("f32", 128, 16), ("f32", 128, 64),
 
 @pytest.mark.parametrize("dtype,dim,block", LONG)
 @pytest.mark.parametrize("heads,lengths,new", [
-    ((4, 2), [140, 130], [151, 3]),     # a tile that is cut along the keys, and few rows beside it
+    ((4, 2), [140, 130], [151, 3]),
     ((4, 1), [140], [300]),
-    ((64, 64), [75], [400]),            # half tiles, as many as fill a chip of 256 compute units uncut
-    ((128, 128), [70], [257]),          # whole tiles
+    ((64, 64), [75], [400]),
+    ((128, 128), [70], [257]),
+    ((128, 128), [70, 3], [401, 2]),    # from here on more than a chip of 256 compute units takes in tiles of 32 rows
+    ((128, 64), [67], [521]),
 ])
 def test_prefill_of_many_rows_over_a_long_cache(dtype, dim, block, heads, lengths, new):
-    """More than 256 rows of a KV head: tiles of keys that every wavefront of a workgroup uses, over more than one batch of 64
-    blocks (lengths in blocks)."""
+    """More than 256 rows of a KV head, over more than one batch of 64 blocks (lengths in blocks): tiles of all kinds, cut along the
+    keys and whole."""
     prefill_case(np.random.default_rng(26), dtype, *heads, dim, block, [n * block - 9 for n in lengths], new, every=37)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "f32"])
 @pytest.mark.parametrize("heads,seqs,longest", [
-    ((7, 1), 140, 900),                 # both kernels cut along the keys, half tiles
-    ((28, 4), 100, 700),                # neither cut, whole tiles
+    ((7, 1), 140, 900),
+    ((28, 4), 100, 700),
+    ((56, 8), 100, 700),                # the longer ones in tiles of 256 rows
+    ((4, 2), 70, 6000),                 # few tiles of very different lengths
 ])
 def test_prefill_of_many_ragged_sequences(dtype, heads, seqs, longest):
     """More sequences than a wavefront looks at in one go, of which some bring many rows, most a few and some none."""
