@@ -8,7 +8,7 @@
 // row: its maximum, sum, limit and rescaling are its own.
 //
 // Bound by the issue of matrix and vector instructions, which two wavefronts of a SIMD overlap only in part: a prompt of 8K tokens,
-// 32 query / 8 KV heads of 128 dims in bf16, takes 594 us (925 TFLOP/s; matrix units busy 36 % of the time, vector units 57 %).
+// 32 query / 8 KV heads of 128 dims in bf16, takes 594 us (925 TFLOP/s; matrix units busy 41 % of the time, vector units 48 %).
 // Without its exponentials it would take 20 us less, without the conversion of bytes 61, without the search for the maximum
 // 50, without the second product 156: no one of them stands out.
 #include <hip/hip_runtime.h>
