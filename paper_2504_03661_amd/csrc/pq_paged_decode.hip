@@ -35,22 +35,30 @@ __device__ inline void load_step(const pq_paged_view &c, const int32_t *table, b
                                  int lane, step_data<D> &s)
 {
     const int k_at = (lane & 15) * D + (lane >> 4) * 16, v_at = lane * 16;
+    // (t is a multiple of 32: both pieces are in one batch)
+    const bool anew = (t >> c.log_block) >= batch.first + 64;
+    if (anew)
+        start_batch(c, table, t >> c.log_block, last_block, h, lane, batch);
+    int at[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int p = t + 16 * i, j = p >> c.log_block;
-        if (j >= batch.first + 64)
-            batch = load_batch(c, table, j, last_block, h, lane);
-        const int at = j - batch.first;
-        const int id = __builtin_amdgcn_readlane(batch.id, at);
-        s.k_scale[i] = lane_of(batch.k_scale, at);
-        s.v_log[i] = lane_of(batch.v_log, at);
-        s.v_inv[i] = lane_of(batch.v_inv, at);
+        const int p = t + 16 * i;
+        at[i] = (p >> c.log_block) - batch.first;
+        const int id = __builtin_amdgcn_readlane(batch.id, at[i]);
         const int64_t base = (((int64_t)id * c.Hkv + h) << c.log_block) * D + (p & ((1 << c.log_block) - 1)) * D;
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) {
             s.k[i][x] = __builtin_nontemporal_load((const u32x4 *)(c.k + base + k_at + 64 * x));
             s.v[i][x] = __builtin_nontemporal_load((const u32x4 *)(c.v + base + v_at + 1024 * x));
         }
+    }
+    if (anew)
+        finish_batch(batch);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        s.k_scale[i] = lane_of(batch.k_scale, at[i]);
+        s.v_log[i] = lane_of(batch.v_log, at[i]);
+        s.v_inv[i] = lane_of(batch.v_inv, at[i]);
     }
 }
 
@@ -134,10 +142,9 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
 
     step_data<D> now, next;
     block_batch batch;
-    if (t0 < t1) {
-        batch = load_batch(a.c, table, t0 >> a.c.log_block, last_block, h, lane);
+    batch.first = -65;
+    if (t0 < t1)
         load_step<D>(a.c, table, batch, last_block, h, t0, lane, now);
-    }
 
     // queries: lane has row `col`, dims 64 x + 16 quad + 0 .. 15, as the instruction's k index takes K's bytes
     half8v q[PARTS][D / 32];

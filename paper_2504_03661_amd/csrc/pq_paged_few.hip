@@ -28,17 +28,17 @@ __device__ inline void load_bytes(const pq_paged_view &c, const int32_t *table, 
                                   step_bytes<D> &s)
 {
     const int col = lane & 31, half = lane >> 5;
+    // (t is a multiple of 32: both pieces are in one batch)
+    const bool anew = (t >> c.log_block) >= batch.first + 64;
+    if (anew)
+        start_batch(c, table, t >> c.log_block, last_block, h, lane, batch);
+    int at[2];
     int64_t base[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-        const int p = t + 16 * i, j = p >> c.log_block;
-        if (j >= batch.first + 64)
-            batch = load_batch(c, table, j, last_block, h, lane);
-        const int at = j - batch.first;
-        const int id = __builtin_amdgcn_readlane(batch.id, at);
-        s.k_scale[i] = lane_of(batch.k_scale, at);
-        s.v_log[i] = lane_of(batch.v_log, at);
-        s.v_inv[i] = lane_of(batch.v_inv, at);
+        const int p = t + 16 * i;
+        at[i] = (p >> c.log_block) - batch.first;
+        const int id = __builtin_amdgcn_readlane(batch.id, at[i]);
         base[i] = (((int64_t)id * c.Hkv + h) << c.log_block) * D + (p & ((1 << c.log_block) - 1)) * D;
     }
     const uint8_t *k = c.k + (col < 16 ? base[0] : base[1]) + (col & 15) * D + 16 * half;
@@ -64,6 +64,14 @@ __device__ inline void load_bytes(const pq_paged_view &c, const int32_t *table, 
                 s.v[i][q][1] = w[1];
             }
         }
+    if (anew)
+        finish_batch(batch);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        s.k_scale[i] = lane_of(batch.k_scale, at[i]);
+        s.v_log[i] = lane_of(batch.v_log, at[i]);
+        s.v_inv[i] = lane_of(batch.v_inv, at[i]);
+    }
 }
 
 template <typename T, int D>
@@ -89,10 +97,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block;
     step_bytes<D> now, next;
     block_batch batch;
-    if (t0 < t1) {
-        batch = load_batch(a.c, table, t0 >> a.c.log_block, last_block, h, lane);
+    batch.first = -65;
+    if (t0 < t1)
         load_bytes<D>(a.c, table, batch, last_block, h, t0, lane, now);
-    }
 
     const int col = lane & 31, half = lane >> 5;
     const bool there = col < tile.rows;

@@ -58,9 +58,9 @@ struct block_batch {
     float k_scale, v_log, v_inv;
 };
 
-__device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane)
+// The first half: block numbers, and the scales on their way, which a block's bytes need not wait for (v_log has V's).
+__device__ inline void start_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane, block_batch &x)
 {
-    block_batch x;
     x.first = first;
     const int j = first + lane;
     int id = j < last ? table[j] : -1;
@@ -70,14 +70,27 @@ __device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *
     x.id = there ? id : 0;
     x.k_scale = 0.0f;  // no such block: every score is -inf, every weight 0
     x.v_log = -INFINITY;
-    x.v_inv = 0.0f;
     if (there) {
         const int64_t at = (int64_t)id * c.Hkv + h;
-        const float v = value_scale(c.v_scale[at]);
         x.k_scale = c.k_scale[at];
-        x.v_log = __log2f(v);
-        x.v_inv = v <= FLT_MAX ? 1.0f / v : 0.0f;  // (a NaN is in v_log: a row that does not see the block adds 0 times this)
+        x.v_log = c.v_scale[at];
     }
+}
+
+// The second half
+__device__ inline void finish_batch(block_batch &x)
+{
+    const bool there = x.v_log != -INFINITY;
+    const float v = value_scale(x.v_log);
+    x.v_log = there ? __log2f(v) : -INFINITY;
+    x.v_inv = there && v <= FLT_MAX ? 1.0f / v : 0.0f;  // (a NaN is in v_log: a row that does not see the block adds 0 times this)
+}
+
+__device__ inline block_batch load_batch(const pq_paged_view &c, const int32_t *table, int first, int last, int h, int lane)
+{
+    block_batch x;
+    start_batch(c, table, first, last, h, lane, x);
+    finish_batch(x);
     return x;
 }
 
