@@ -345,7 +345,8 @@ int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_
  * tok_len[b] - 1 of q are the last tok_len[b] tokens of sequence b, and row i of them attends over the first
  * seq_len[b] - tok_len[b] + i + 1 tokens (a row for which that is not positive gets zeros).
  *
- *   n_tokens             rows of q and out, >= the end of the last sequence's rows
+ *   n_tokens             rows of q and out, >= the end of the last sequence's rows (the kernels are chosen by what they are
+ *                        on average: a call padded to many times its tokens is right, but slower)
  *   q                    as in pq_paged_decode, row t at t * q_stride elements
  *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
  *   tok_start, tok_len   device int32, as pq_paged_plan gives them (rows from n_tokens on are left out, a sequence whose

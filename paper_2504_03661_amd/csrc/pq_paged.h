@@ -132,13 +132,14 @@ template <typename T> struct __align__(16) paged_row8 {
     T x[8];
 };
 
-template <typename T> __device__ inline void paged_load8(const T *p, float *x)
+template <typename T> __device__ inline void paged_up8(const paged_row8<T> &r, float *x)
 {
-    const paged_row8<T> r = *(const paged_row8<T> *)p;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         x[i] = paged_elem<T>::up(r.x[i]);
 }
+
+template <typename T> __device__ inline void paged_load8(const T *p, float *x) { paged_up8(*(const paged_row8<T> *)p, x); }
 
 template <typename T> __device__ inline void paged_store8(T *p, const float *x)
 {

@@ -12,7 +12,9 @@
 // whatever the lengths are.  Every workgroup works the cut out for itself from the lengths.  A sequence of several
 // chunks is put together by the workgroup that finishes last (pq_device_utils.h, exchange of split partials).
 //
-// Bound by HBM: 2 d bytes per token and KV head.
+// Bound by HBM, 2 d bytes per token and KV head: 8 sequences x 32 heads x 32K tokens in fp16 336 us, 6.4 TB/s.  Short calls by
+// latency: a launch, lengths, block numbers, the bytes, the merge, each a trip to memory that waits for the one before — the
+// queries and the scales travel beside them (32 heads x 1000 tokens 6.6 us).
 #include <hip/hip_runtime.h>
 
 #include "pq_paged_tile.h"
@@ -140,24 +142,26 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     const int32_t *table = a.c.table + (int64_t)p.b * a.c.max_blocks;
     const int last_block = (p.len + (1 << a.c.log_block) - 1) >> a.c.log_block;
 
+    // queries: lane has row `col`, dims 64 x + 16 quad + 0 .. 15, as the instruction's k index takes K's bytes
+    paged_row8<T> row[D / 32];
+    const T *src = (const T *)a.q + (int64_t)p.b * a.q_stride + (int64_t)(head0 + (col < rows ? col : 0)) * D + quad * 16;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+        row[i] = *(const paged_row8<T> *)(src + 64 * (i >> 1) + 8 * (i & 1));
     step_data<D> now, next;
     block_batch batch;
     batch.first = -65;
     if (t0 < t1)
         load_step<D>(a.c, table, batch, last_block, h, t0, lane, now);
 
-    // queries: lane has row `col`, dims 64 x + 16 quad + 0 .. 15, as the instruction's k index takes K's bytes
     half8v q[PARTS][D / 32];
     float per_score;  // what a dot product of codes is multiplied by, but for the block's scale
     {
         float x[D / 4];
-        const T *src = (const T *)a.q + (int64_t)p.b * a.q_stride + (int64_t)(head0 + (col < rows ? col : 0)) * D + quad * 16;
         float high = 0.0f;
 #pragma unroll
-        for (int i = 0; i < D / 64; ++i) {
-            paged_load8(src + 64 * i, x + 16 * i);
-            paged_load8(src + 64 * i + 8, x + 16 * i + 8);
-        }
+        for (int i = 0; i < D / 32; ++i)
+            paged_up8(row[i], x + 8 * i);
 #pragma unroll
         for (int i = 0; i < D / 4; ++i)
             high = fmaxf(high, fabsf(x[i]));
@@ -340,7 +344,7 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
 
 // Chunks are as many as keep the chip busy, PER_CU workgroups a compute unit (8 x 32 heads x 32K: 348 us with one, 336 with two,
 // 342 with three; 32 query / 8 KV heads x 128K 53, 54 and 59), and not more than the last workgroup reads in a few
-// microseconds (16 query heads of one KV head x 100K: 46 us with up to 128, 40 with 64).
+// microseconds (16 query heads of one KV head x 100K: 46 us with up to 128, 40 with 64; 36 since scales are not waited for).
 pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu)
 {
     constexpr int PER_CU = 2, MOST = 64;
