@@ -203,15 +203,15 @@ __device__ inline void step_32(row_state<S, PARTS> &r, const tile_lds<S> &next, 
 #pragma unroll
             for (int j = 0; j < 8; j += 2) {
                 const float x = __builtin_amdgcn_exp2f(e[n][8 * i + j]), y = __builtin_amdgcn_exp2f(e[n][8 * i + j + 1]);
+                // (before they are rounded: a weight is as large as its block's values are, and one that fp16 has no
+                // number for counts in the sum as much as any other)
+                sum += x + y;
                 const half2v both = {(_Float16)x, (_Float16)y};
                 w.w[n][0][i][j] = both.x;
                 w.w[n][0][i][j + 1] = both.y;
                 if (PARTS == 2) {
-                    sum += x + y;
                     w.w[n][PARTS - 1][i][j] = (_Float16)(x - (float)both.x);
                     w.w[n][PARTS - 1][i][j + 1] = (_Float16)(y - (float)both.y);
-                } else {
-                    sum = __builtin_amdgcn_fdot2(both, half2v{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
                 }
             }
             r.l[n] = fmaf(sum, v_inv[i], r.l[n]);

@@ -6,8 +6,11 @@
 // parts, 22 bits.  Products and sums are fp32.  A block's key scale multiplies the finished dot product; its value scale goes into
 // the weights' exponent:
 //     s_t = log2(e) scale q.k_t + log2(v_scale_t),   w_t = 2^(s_t - m + 13),   out = sum_t w_t code_t / sum_t w_t / v_scale_t
-// with m near the largest s_t, so that the weights — rounded to fp16 (fp32 contexts: to two parts) — keep 11 bits down to 2^-27 of
-// the largest and never leave fp16's range.
+// with m near the largest s_t, so that the weights that are multiplied by codes — rounded to fp16 (fp32 contexts: to two parts): a
+// matrix instruction in fp32 has a sixteenth of the rate — keep 11 bits down to 2^-27 of the largest and never leave fp16's range.
+// That is all the first sum needs, in which a weight counts by the size of its values.  In the second it counts by the softmax
+// alone, however small its values are (a block of zeros has the scale 2^-40): that sum is taken of the weights in fp32, before they are
+// rounded.  There they reach down to 2^-139 of the largest.
 #pragma once
 
 #include <cfloat>
