@@ -47,11 +47,12 @@ __device__ inline half8v codes8(uint32_t w0, uint32_t w1)
 // A block's value scale: never below 2^-40, which a block that nothing was written to would be (a NaN stays).
 __device__ inline float value_scale(float v) { return v < 0x1p-40f ? 0x1p-40f : v; }
 
-// the exponent by which a row of queries is scaled, from its largest |element|
+// The exponent by which a row of queries is scaled, from its largest |element|: that has 13 afterwards, subnormal or not.  (A row of
+// zeros gets the largest there is: no scale then makes anything but 0 of its scores.)
 __device__ inline int query_exponent(float largest)
 {
-    const int e = (int)(__float_as_uint(largest) >> 23);  // 0: no row element above the subnormal numbers
-    return e == 0 ? 0 : 13 + 127 - e;
+    const uint32_t bits = __float_as_uint(largest);
+    return (bits >> 23) != 0 ? 13 + 127 - (int)(bits >> 23) : 13 + 149 - 31 + __builtin_clz(bits | 1u);
 }
 
 // What a lane keeps of 64 blocks in a row of a sequence
