@@ -335,7 +335,7 @@ int pq_paged_read(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_rows, const uint8
  * out = sum_t softmax_t(scale * q . k_t) v_t.
  *
  *   q            device, row b at b * q_stride elements, [Hq][d] dtype there (q_stride >= Hq * d)
- *   scale        as in pq_attn_decode
+ *   scale        finite, as is its product with log2(e) in fp32: up to 2.358e38 (PQ_ERR_SHAPE otherwise)
  *   out          device [n_seqs][Hq][d] dtype; a sequence without tokens gets a row of zeros */
 int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_stride, const uint8_t *k_cache,
                     const uint8_t *v_cache, const float *k_scale, const float *v_scale, const int32_t *block_table,

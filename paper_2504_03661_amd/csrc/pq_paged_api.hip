@@ -1,6 +1,7 @@
 // C ABI of the paged 8-bit cache: argument checks, context life cycle, launch plumbing.
 #include <hip/hip_runtime.h>
 
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -84,7 +85,7 @@ int attend(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const void *q, i
 {
     if (!aligned(q) || !aligned(out) || !aligned(c.k) || !aligned(c.v) || !stride_fits(ctx, q_stride, ctx->cfg.n_q_heads))
         return PQ_ERR_SHAPE;
-    if (!(fabsf(scale) <= 3.0e38f))  // NaN or infinite
+    if (!(fabsf(scale * LOG2E) <= FLT_MAX))  // NaN or infinite, or so in what the kernels multiply by
         return PQ_ERR_SHAPE;
     device_guard guard(ctx->cfg.device);
     if (!guard.ok)

@@ -48,3 +48,16 @@ def test_queries_of_zeros_under_a_large_scale(path, dtype):
     p.put("k")
     scale = float(np.float32(1e38))
     p.check(attend(p, path, scale), scale)
+
+
+@pytest.mark.parametrize("path", PATHS)
+def test_scales_that_have_no_logarithm_to_two(path):
+    """scale * log2(e) has to be a number: what is not is refused, what just is gives the mean for queries of zeros."""
+    p = prompt(np.random.default_rng(43), path, "f32", 700)
+    p.q, p.values[:] = torch.zeros_like(p.q), 0.0
+    for scale in (2.37e38, -3e38, 3.4e38):
+        with pytest.raises(pq.PQAttnError) as e:
+            attend(p, path, scale)
+        assert e.value.status == -2
+    scale = float(np.float32(-2.35e38))
+    p.check(attend(p, path, scale), scale)
