@@ -332,7 +332,10 @@ int pq_paged_read(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_rows, const uint8
                   const int32_t *first, void *out_k, void *out_v, void *hip_stream);
 
 /* Attention of one query token per sequence over all its seq_len[b] tokens (its own, appended before, among them):
- * out = sum_t softmax_t(scale * q . k_t) v_t.
+ * out = sum_t softmax_t(scale * q . k_t) v_t, with scores, weights and sums of both in fp32's range.  A weight is kept in units of the
+ * largest v_scale * softmax of its row, down to 2^-126 of it: with values up to 2^48 in size every token counts whose softmax
+ * weight is at least 2^-45 of the largest, also one of a block of zeros (scale 2^-40).  Larger values (bf16, fp32) take from that,
+ * each doubling of them a factor of 2 for the tokens of the smallest blocks.
  *
  *   q            device, row b at b * q_stride elements, [Hq][d] dtype there (q_stride >= Hq * d)
  *   scale        finite, as is its product with log2(e) in fp32: up to 2.358e38 (PQ_ERR_SHAPE otherwise)

@@ -10,7 +10,7 @@
 // matrix instruction in fp32 has a sixteenth of the rate — keep 11 bits down to 2^-27 of the largest and never leave fp16's range.
 // That is all the first sum needs, in which a weight counts by the size of its values.  In the second it counts by the softmax
 // alone, however small its values are (a block of zeros has the scale 2^-40): that sum is taken of the weights in fp32, before they are
-// rounded.  There they reach down to 2^-139 of the largest.
+// rounded.  There they count down to 2^-126 of the largest (the range of the factors by which sums follow the maximum).
 #pragma once
 
 #include <cfloat>

@@ -61,3 +61,17 @@ def test_scales_that_have_no_logarithm_to_two(path):
         assert e.value.status == -2
     scale = float(np.float32(-2.35e38))
     p.check(attend(p, path, scale), scale)
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_far_larger_than_those_beside_them(path, dtype):
+    """Values up to 2^64 in every second block, zeros in the others.  Their scales are 2^97 apart, which leaves 2^-29 of 2^-126 for the
+    smallest softmax weight that counts (scores here spread over some 8: 2^-12)."""
+    p = prompt(np.random.default_rng(42), path, dtype, 700)
+    m = p.c.model["v"]
+    m.scale *= np.float32(2.0 ** 62)
+    zero = p.c.table[0][1::2]
+    m.codes[zero], m.scale[zero] = 0, np.float32(2.0 ** -40)
+    p.put("v")
+    p.check(attend(p, path, 0.1), 0.1)
