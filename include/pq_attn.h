@@ -353,7 +353,9 @@ int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_
  *   q                    as in pq_paged_decode, row t at t * q_stride elements
  *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
  *   tok_start, tok_len   device int32, as pq_paged_plan gives them (rows from n_tokens on are left out, a sequence whose
- *                        first row is outside [0, n_tokens) altogether; rows that two sequences claim hold nobody's result)
+ *                        first row is outside [0, n_tokens) altogether; rows that two sequences claim hold nobody's result,
+ *                        and where the sequences claim more than n_tokens rows in all, bit 2 of the device error word is
+ *                        set and none of the call's rows is to be used)
  *   out                  device [n_tokens][Hq][d] dtype; rows of no sequence are left as they were
  *
  * 0 <= n_tokens <= max_tokens; 0 does nothing. */
@@ -362,7 +364,8 @@ int pq_paged_prefill(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const 
                      const int32_t *block_table, const int32_t *seq_len, const int32_t *tok_start, const int32_t *tok_len,
                      float scale, void *out, void *hip_stream);
 
-/* As pq_attn_device_error.  Bit 0: pq_paged_plan refused a request; bit 1: a block number or slot outside the cache. */
+/* As pq_attn_device_error.  Bit 0: pq_paged_plan refused a request; bit 1: a block number or slot outside the cache; bit 2: the
+ * sequences of a pq_paged_prefill claimed more rows than it had. */
 int pq_paged_device_error(pq_paged_ctx *ctx, uint32_t *flags /* host */);
 
 /* Static, never NULL. */

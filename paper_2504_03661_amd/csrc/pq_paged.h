@@ -12,6 +12,7 @@
 #define PQ_PAGED_MAX_TOKENS (1 << 20)
 #define PQ_PAGED_ERRFLAG_REFUSED 1u
 #define PQ_PAGED_ERRFLAG_RANGE 2u
+#define PQ_PAGED_ERRFLAG_CLAIMS 4u
 
 // how pq_paged_decode's workgroups are cut out, and what they exchange through
 struct pq_paged_decode_plan {

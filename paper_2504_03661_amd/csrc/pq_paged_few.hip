@@ -84,6 +84,11 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv, entry = blockIdx.x / a.c.Hkv;
+    if (blockIdx.x == gridDim.x - 1) {  // (one more than the list has)
+        if (wave == 0)
+            check_claims(a, lane);
+        return;
+    }
     work_place p;
     if (!find_work(a, few_rule(w), entry, lane, p))
         return;
@@ -356,7 +361,7 @@ hipError_t pq_launch_paged_prefill(const pq_paged_ctx *ctx, const pq_paged_attn_
         w.budget = 0;
     const int dtype = ctx->cfg.dtype, dim = ctx->cfg.head_dim;
     if (w.few_rows > 0) {
-#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.budget) * a.c.Hkv)), dim3(THREADS), 0, s, a, w)
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_few_kernel<T, D>), dim3((unsigned)((few_tiles + w.budget) * a.c.Hkv) + 1), dim3(THREADS), 0, s, a, w)
         PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH
     }

@@ -231,6 +231,11 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv, entry = blockIdx.x / a.c.Hkv;
+    if (blockIdx.x == gridDim.x - 1) {  // (one more than the list has)
+        if (wave == 0)
+            check_claims(a, lane);
+        return;
+    }
     work_place p;
     if (!find_work(a, tile_rule(w), entry, lane, p))
         return;
@@ -378,7 +383,7 @@ hipError_t pq_launch_paged_tiles(const pq_paged_attn_args &a, const pq_paged_pre
 #define LAUNCH(T, D)                                                                                                          \
     do {                                                                                                                      \
         using S = shape<D, 1, PQ_PAGED_TILE_ROWS / 32, 64 * 128 / D>;                                                         \
-        hipLaunchKernelGGL((pq_paged_prefill_kernel<T, S>), dim3((unsigned)(tiles * a.c.Hkv)), dim3(S::THREADS), 0, s, a, w); \
+        hipLaunchKernelGGL((pq_paged_prefill_kernel<T, S>), dim3((unsigned)(tiles * a.c.Hkv) + 1), dim3(S::THREADS), 0, s, a, w); \
     } while (0)
     PQ_PAGED_BY_TYPE(dtype, dim, LAUNCH);
 #undef LAUNCH

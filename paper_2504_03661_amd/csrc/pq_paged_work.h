@@ -28,6 +28,21 @@ __device__ inline int rows_there(const pq_paged_attn_args &a, int b, int &start,
     return n < a.n_tokens - start ? n : a.n_tokens - start;
 }
 
+// The grids are as large as sequences need whose rows are apart.  Where rows are claimed twice the list of work may be longer, and
+// its end is left out; where all claims together are no more than the tensors have rows it is not.  One workgroup, of
+// which the list asks nothing, says so.
+__device__ inline void check_claims(const pq_paged_attn_args &a, int lane)
+{
+    int claimed = 0;  // (limited so that 64 lanes' sum fits 32 bits and decides the same)
+    for (int b = lane; b < a.n_seqs; b += 64) {
+        int start, asked;
+        claimed += rows_there(a, b, start, asked);
+        claimed = claimed > a.n_tokens ? a.n_tokens + 1 : claimed;
+    }
+    if (__builtin_amdgcn_readlane(lane_scan(claimed), 63) > a.n_tokens && lane == 0)
+        paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_CLAIMS);
+}
+
 // Which sequences a kernel takes, and how it cuts them up
 struct work_rule {
     int least, most;  // rows (tokens times query heads of a KV head) of its sequences

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2504_03661_amd as pq
-from tests.paged_inputs import TORCH
+from tests.paged_inputs import TORCH, Filled, check, context, dev, rounded
 from tests.test_gpu_paged_tiles import DIM, HEADS, Prompt
 
 pytestmark = pytest.mark.gpu
@@ -75,3 +75,47 @@ def test_values_far_larger_than_those_beside_them(path, dtype):
     m.codes[zero], m.scale[zero] = 0, np.float32(2.0 ** -40)
     p.put("v")
     p.check(attend(p, path, 0.1), 0.1)
+
+
+CLAIMS = {       # rows claimed by each sequence: first, number; rows of the tensors; whether they are more in all
+    "apart": ([(0, 30), (30, 10)], 40, False),
+    "apart, cut off by the tensors' end": ([(0, 30), (30, 2 ** 31 - 1)], 40, False),
+    "outside the tensors": ([(0, 40), (40, 5), (-3, 9), (2 ** 31 - 1, 1)], 40, False),
+    "twice, and others by nobody": ([(0, 10), (0, 10), (20, 10)], 40, False),
+    "one row twice": ([(0, 30), (29, 11)], 40, True),
+    "all by sixty": ([(0, 40)] * 60, 40, True),
+    "as many as numbers reach": ([(0, 2 ** 31 - 1)] * 300, 50, True),
+}
+
+
+@pytest.mark.parametrize("what", CLAIMS)
+@pytest.mark.parametrize("heads", [2, 128], ids=["few rows", "many rows"])
+def test_rows_claimed_twice_are_reported(what, heads):
+    """Bit 2 where the claims are more than there are rows; else a sequence whose rows nobody else claims gets what is right."""
+    claims, tokens, more = CLAIMS[what]
+    more_rows = 1 if heads == 2 else 30                      # 128 heads: 300 and more rows a sequence, enough for tiles of 256
+    claims = [(first * more_rows if 0 <= first < 2 ** 20 else first, min(n * more_rows, 2 ** 31 - 1)) for first, n in claims]
+    tokens *= more_rows
+    rng = np.random.default_rng(44)
+    c = Filled(rng, np.array([500] * 3), heads, DIM, 16)
+    c.table, c.lengths = c.table[np.arange(len(claims)) % 3], np.full(len(claims), 500)     # (sequences that share their blocks)
+    c.block_table, c.seq_len = dev(c.table), dev(c.lengths)
+    ctx = context("f16", heads, heads, DIM, 16, c.n_blocks, c.width, len(claims), tokens)
+    q, values = rounded(rng.standard_normal((tokens, heads, DIM)), "f16")
+    room = torch.full((tokens + 8, heads, DIM), 7.0, dtype=torch.float16, device="cuda")
+    out = room[4:-4]
+    first, n = (dev([x[i] for x in claims] + [0]) for i in (0, 1))
+    pq.pq_paged_prefill(ctx.handle, len(claims), tokens, q.cuda(), heads * DIM, *c.args(), first, n, 0.1, out)
+    assert pq.pq_paged_device_error(ctx.handle) == (4 if more else 0)
+    assert (room[:4] == 7.0).all() and (room[-4:] == 7.0).all()
+    if more:
+        return
+    claimed = np.zeros(tokens, int)
+    ends = [min(first + n, tokens) if 0 <= first < tokens else first for first, n in claims]
+    for (first, _), end in zip(claims, ends):
+        claimed[first:max(first, end)] += 1 if 0 <= first < tokens else 0
+    assert (out[claimed == 0] == 7.0).all()
+    for b, ((first, n), end) in enumerate(zip(claims, ends)):
+        if 0 <= first < tokens and (claimed[first:end] == 1).all():
+            i = np.arange(end - first)[::-57][::-1]
+            check(out[first + i], *c.attention(values[first + i], b, 0.1, 500 - n + i + 1), "f16", DIM, f"sequence {b}")
