@@ -122,7 +122,7 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     constexpr int PARTS = SPLIT ? 2 : 1;
     constexpr int DT = D / 16;
     __shared__ float part[WAVES][ROWS][D + 4];
-    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS], row_m[ROWS], row_l[ROWS];
+    __shared__ float wave_base[WAVES][ROWS], wave_l[WAVES][ROWS], row_base[ROWS], row_l[ROWS];
     __shared__ int last_one;
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
 #pragma unroll
     for (int i = 0; i < DT; ++i)
         o[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    float m = LOWEST, l = 0.0f;
+    float base = LOWEST, l = 0.0f;
     for (int t = t0; t < t1; t += STEP) {
         const bool more = t + STEP < t1;
         if (more)
@@ -214,17 +214,16 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
 #pragma unroll
         for (int i = 1; i < 8; ++i)
             high = fmaxf(high, s[i]);
-        if (__ballot(high > m + MAX_SLACK) != 0) {
+        if (__ballot(high - base > MOST_BITS) != 0) {
             high = fmaxf(high, __shfl_xor(high, 16, 64));
             high = fmaxf(high, __shfl_xor(high, 32, 64));
-            const float moved = fmaxf(m, high), down = __builtin_amdgcn_exp2f(m - moved);
-            m = moved;
+            const float moved = fmaxf(base, weight_base(high)), down = __builtin_amdgcn_exp2f(base - moved);
+            base = moved;
             l *= down;
 #pragma unroll
             for (int i = 0; i < DT; ++i)
                 o[i] *= down;
         }
-        const float base = m - WEIGHT_BITS;
         half8v weights[PARTS];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -254,7 +253,7 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     if (quad == 0) {
-        wave_m[wave][col] = m;
+        wave_base[wave][col] = base;
         wave_l[wave][col] = l;
     }
 #pragma unroll
@@ -263,17 +262,17 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     __syncthreads();
     if (threadIdx.x < ROWS) {
         const int r = threadIdx.x;
-        float top = wave_m[0][r], sum = 0.0f;
+        float top = wave_base[0][r], sum = 0.0f;
 #pragma unroll
         for (int i = 1; i < WAVES; ++i)
-            top = fmaxf(top, wave_m[i][r]);
+            top = fmaxf(top, wave_base[i][r]);
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) {
-            const float down = __builtin_amdgcn_exp2f(wave_m[i][r] - top);
+            const float down = __builtin_amdgcn_exp2f(wave_base[i][r] - top);
             sum = fmaf(wave_l[i][r], down, sum);
-            wave_m[i][r] = down;
+            wave_base[i][r] = down;
         }
-        row_m[r] = top;
+        row_base[r] = top;
         row_l[r] = sum;
     }
     __syncthreads();
@@ -287,8 +286,8 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
         float x = 0.0f, y = 0.0f;
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) {
-            x = fmaf(part[k][r][d], wave_m[k][r], x);
-            y = fmaf(part[k][r][d + 1], wave_m[k][r], y);
+            x = fmaf(part[k][r][d], wave_base[k][r], x);
+            y = fmaf(part[k][r][d + 1], wave_base[k][r], y);
         }
         if (p.chunks == 1) {
             const float sum = row_l[r], by = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -301,7 +300,7 @@ __global__ __launch_bounds__(THREADS, 2) void pq_paged_decode_kernel(pq_paged_at
     if (p.chunks == 1)
         return;
     if (threadIdx.x < rows)
-        publish(mine + threadIdx.x * (D + 2), row_m[threadIdx.x], row_l[threadIdx.x]);
+        publish(mine + threadIdx.x * (D + 2), row_base[threadIdx.x], row_l[threadIdx.x]);
     publish_wait();
     __syncthreads();
     unsigned int *ticket = w.tickets + slot0;

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     constexpr bool SPLIT = sizeof(T) == 4;  // two fp16 parts of queries and weights
     constexpr int PARTS = SPLIT ? 2 : 1, DT = D / 32;
     __shared__ float part[WAVES][ROWS][D + 4];
-    __shared__ float wave_m[WAVES][ROWS], wave_l[WAVES][ROWS], row_m[ROWS], row_l[ROWS];
+    __shared__ float wave_base[WAVES][ROWS], wave_l[WAVES][ROWS], row_base[ROWS], row_l[ROWS];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv, entry = blockIdx.x / a.c.Hkv;
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
 #pragma unroll
         for (int j = 0; j < 16; ++j)
             o[i][j] = 0.0f;
-    float m = LOWEST, l = 0.0f;
+    float base = LOWEST, l = 0.0f;
     for (int t = t0; t < t1; t += STEP) {
         const bool more = t + STEP < t1;
         if (more)
@@ -180,10 +180,10 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
 #pragma unroll
         for (int j = 1; j < 16; ++j)
             high = fmaxf(high, s[j]);
-        if (__ballot(high > m + MAX_SLACK) != 0) {
+        if (__ballot(high - base > MOST_BITS) != 0) {
             high = fmaxf(high, __shfl_xor(high, 32, 64));
-            const float moved = fmaxf(m, high), down = __builtin_amdgcn_exp2f(m - moved);
-            m = moved;
+            const float moved = fmaxf(base, weight_base(high)), down = __builtin_amdgcn_exp2f(base - moved);
+            base = moved;
             l *= down;
 #pragma unroll
             for (int i = 0; i < DT; ++i)
@@ -191,7 +191,6 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
                 for (int j = 0; j < 16; ++j)
                     o[i][j] *= down;
         }
-        const float base = m - WEIGHT_BITS;
         half8v weights[PARTS][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -222,7 +221,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     // the wavefronts' parts
     l += __shfl_xor(l, 32, 64);
     if (half == 0) {
-        wave_m[wave][col] = m;
+        wave_base[wave][col] = base;
         wave_l[wave][col] = l;
     }
 #pragma unroll
@@ -235,17 +234,17 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
     __syncthreads();
     if (threadIdx.x < ROWS) {
         const int r = threadIdx.x;
-        float top = wave_m[0][r], sum = 0.0f;
+        float top = wave_base[0][r], sum = 0.0f;
 #pragma unroll
         for (int i = 1; i < WAVES; ++i)
-            top = fmaxf(top, wave_m[i][r]);
+            top = fmaxf(top, wave_base[i][r]);
 #pragma unroll
         for (int i = 0; i < WAVES; ++i) {
-            const float down = __builtin_amdgcn_exp2f(wave_m[i][r] - top);
+            const float down = __builtin_amdgcn_exp2f(wave_base[i][r] - top);
             sum = fmaf(wave_l[i][r], down, sum);
-            wave_m[i][r] = down;
+            wave_base[i][r] = down;
         }
-        row_m[r] = top;
+        row_base[r] = top;
         row_l[r] = sum;
     }
     __syncthreads();
@@ -255,8 +254,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
         float x = 0.0f, y = 0.0f;
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) {
-            x = fmaf(part[k][r][d], wave_m[k][r], x);
-            y = fmaf(part[k][r][d + 1], wave_m[k][r], y);
+            x = fmaf(part[k][r][d], wave_base[k][r], x);
+            y = fmaf(part[k][r][d + 1], wave_base[k][r], y);
         }
         if (tile.pieces == 1) {
             const float by = row_l[r] == 0.0f ? 0.0f : 1.0f / row_l[r];
@@ -267,7 +266,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
         } else {
             *(float2 *)(to + r * (D + 2) + 2 + d) = make_float2(x, y);
             if (d == 0)
-                *(float2 *)(to + r * (D + 2)) = make_float2(row_m[r], row_l[r]);
+                *(float2 *)(to + r * (D + 2)) = make_float2(row_base[r], row_l[r]);
         }
     }
 }

@@ -87,7 +87,8 @@ __device__ inline void store_keys(tile_lds<S> &lds, const block_batch &batch, in
 template <typename S, int PARTS> struct row_state {
     half8v q[S::NT][PARTS][S::D / 16];
     f32x16 o[S::D / 32][S::NT];
-    float per_score[S::NT], m[S::NT], l[S::NT];
+    float per_score[S::NT], base[S::NT], l[S::NT];
+    float most[S::NT];  // the exponent of a weight above which the base is moved
     int sees[S::NT];  // keys that the row attends over
 };
 
@@ -149,12 +150,14 @@ __device__ inline void step_32(row_state<S, PARTS> &r, const tile_lds<S> &next, 
         v_log[i] = now.v_log[2 * u + i];
         v_inv[i] = now.v_inv[2 * u + i];
     }
-    // exponents of the weights, s - m + 13: one fma of a dot product, of which the largest decides whether m stays
+    // Exponents of the weights, s - base: one fma of a dot product, of which the largest decides whether the base stays.  The fma does
+    // not round the product, as the score was that became the base.  Beyond 2^22 that is a matter of half a unit and more:
+    // there every step goes the other way, by scores that are rounded, so that scores alike have weights alike.
     float e[NT][16];
     auto exponents = [&](int n) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float by = r.per_score[n] * k_scale[i], off = v_log[i] - (r.m[n] - WEIGHT_BITS);
+            const float by = r.per_score[n] * k_scale[i], off = v_log[i] - r.base[n];
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 e[n][8 * i + j] = fmaf(dot[n][8 * i + j], by, off);
@@ -174,24 +177,27 @@ __device__ inline void step_32(row_state<S, PARTS> &r, const tile_lds<S> &next, 
     bool moves = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
-        moves |= exponents(n) > WEIGHT_BITS + MAX_SLACK;
+        moves |= exponents(n) > r.most[n];
     if (__ballot(moves) != 0) {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            // the largest score itself (an m that has seen nothing is too large to be subtracted and added again)
-            const float was = r.m[n];
-            r.m[n] = WEIGHT_BITS;
+            // (from the scores themselves: the base of a row that has seen nothing is too large to be subtracted and added again)
+            const float was = r.base[n];
+            r.base[n] = 0.0f;
             float high = exponents(n);
             high = fmaxf(high, __shfl_xor(high, 32, 64));
-            const float moved = fmaxf(was, high), down = __builtin_amdgcn_exp2f(was - moved);
-            r.m[n] = moved;
+            const float base = fmaxf(was, weight_base(high)), down = __builtin_amdgcn_exp2f(was - base);
+            r.base[n] = base;
+            r.most[n] = fabsf(base) < 0x1p22f ? MOST_BITS : -INFINITY;
             r.l[n] *= down;
 #pragma unroll
             for (int i = 0; i < D / 32; ++i)
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     r.o[i][n][j] *= down;
-            exponents(n);
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                e[n][j] -= base;
         }
     }
     dots_32<S, PARTS>(r, next, next_u, col, half, dot_next);
@@ -254,7 +260,8 @@ __global__ __launch_bounds__(S::THREADS, 2) void pq_paged_prefill_kernel(pq_page
         head[n] = there ? r - token[n] * a.G : 0;
         const int sees = there ? past + token[n] + 1 : 0;
         rows.sees[n] = sees < k1 ? sees : k1;
-        rows.m[n] = LOWEST;
+        rows.base[n] = LOWEST;
+        rows.most[n] = MOST_BITS;
         rows.l[n] = 0.0f;
 #pragma unroll
         for (int i = 0; i < DT; ++i)

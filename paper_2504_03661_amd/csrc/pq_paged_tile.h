@@ -5,8 +5,8 @@
 // fewer bits wide (fp16, bf16) stays exact down to 2^-27 of the row's largest element; fp32 rows are split into two fp16
 // parts, 22 bits.  Products and sums are fp32.  A block's key scale multiplies the finished dot product; its value scale goes into
 // the weights' exponent:
-//     s_t = log2(e) scale q.k_t + log2(v_scale_t),   w_t = 2^(s_t - m + 13),   out = sum_t w_t code_t / sum_t w_t / v_scale_t
-// with m near the largest s_t, so that the weights that are multiplied by codes — rounded to fp16 (fp32 contexts: to two parts): a
+//     s_t = log2(e) scale q.k_t + log2(v_scale_t),   w_t = 2^(s_t - base),   out = sum_t w_t code_t / sum_t w_t / v_scale_t
+// with the base 13 to 15 below the largest s_t, so that the weights that are multiplied by codes — rounded to fp16 (fp32 contexts: to two parts): a
 // matrix instruction in fp32 has a sixteenth of the rate — keep 11 bits down to 2^-27 of the largest and never leave fp16's range.
 // That is all the first sum needs, in which a weight counts by the size of its values.  In the second it counts by the softmax
 // alone, however small its values are (a block of zeros has the scale 2^-40): that sum is taken of the weights in fp32, before they are
@@ -25,9 +25,13 @@ typedef _Float16 half4v __attribute__((ext_vector_type(4)));
 typedef _Float16 half8v __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr float WEIGHT_BITS = 13.0f;  // log2 of the largest weight, before m's slack
-constexpr float LOWEST = -3.0e38f;     // m of a row that has seen nothing
-constexpr float MAX_SLACK = 2.0f;     // m is moved when a score is more than this above it: weights stay below 2^15
+constexpr float WEIGHT_BITS = 13.0f;  // log2 of the weight of the largest score when it sets a row's base
+constexpr float MOST_BITS = 15.0f;    // .. and of one above which the base is moved: fp16 holds what is below 2^16
+constexpr float LOWEST = -FLT_MAX;     // the base of a row that has seen nothing
+
+// What a row's weights are measured from, 2^(s - base), if its largest score is s: 13 below it, and from 2^22 on, where s less 13
+// is rounded — by more than fp16 leaves room for soon —, s itself.
+__device__ inline float weight_base(float s) { return fabsf(s) < 0x1p22f ? s - WEIGHT_BITS : s; }
 
 // Four bytes (code + 128) as fp16 codes: 0x6400 | byte is 1024 + byte, and 1152 less is the code.
 __device__ inline half4v codes4(uint32_t w)

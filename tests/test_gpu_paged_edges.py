@@ -1,10 +1,12 @@
 """Numbers at the ends of their ranges through each of the paged cache's attention kernels: decode, and prefill's two."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 import paper_2504_03661_amd as pq
-from tests.paged_inputs import TORCH, Filled, check, context, dev, rounded
+from tests.paged_inputs import HALF_STEP, TORCH, Filled, check, context, dev, rounded
 from tests.test_gpu_paged_tiles import DIM, HEADS, Prompt
 
 pytestmark = pytest.mark.gpu
@@ -119,3 +121,51 @@ def test_rows_claimed_twice_are_reported(what, heads):
         if 0 <= first < tokens and (claimed[first:end] == 1).all():
             i = np.arange(end - first)[::-57][::-1]
             check(out[first + i], *c.attention(values[first + i], b, 0.1, 500 - n + i + 1), "f16", DIM, f"sequence {b}")
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("power", [12, 23, 40, 120])
+def test_scores_far_beyond_the_numbers_below_one(path, dtype, power):
+    """Where a row's largest score is further above the next than both can be off, its answer is that token's value: off by the rounding of
+    its weight (fp32: in two parts), 2^-19 for the sum and half a step of the output."""
+    p = prompt(np.random.default_rng(45), path, dtype, 700)
+    out = attend(p, path, 2.0 ** power).double().cpu().numpy()
+    assert np.isfinite(out).all()
+    k, v = (p.c.model[kind].rows(p.c.table[0], 700)[0] for kind in "kv")
+    decided = 0
+    rows = np.arange(p.new)[::-37]
+    for r in rows:
+        for h in range(HEADS):
+            t = k[h, :p.sees(r)] @ p.values[r, h]
+            off = (DIM + 16) * 2.0 ** -24 * (np.abs(k[h]) @ np.abs(p.values[r, h])).max()
+            best = int(t.argmax())
+            gap = t[best] - np.delete(t, best).max()
+            if gap > 4 * off and gap * 2.0 ** power > 60:
+                decided += 1
+                want = v[h, best]
+                allowed = np.abs(want) * (HALF_STEP[dtype] * 1.01 + (2.0 ** -21 if dtype == "f32" else 2.0 ** -11) + 2.0 ** -19) + 2.0 ** -25
+                assert (np.abs(out[r, h] - want) <= allowed).all(), (r, h)
+    assert decided > 0.9 * HEADS * len(rows)
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("at", [-3.3e38, 3.3e38, 2.0 ** 22, -2.0 ** 22 + 3.0, 2.0 ** 26 + 24.0, -2.0 ** 27])
+def test_scores_all_alike_far_from_zero(path, at):
+    """Every token has the score `at` (in base two), or nearly, so every row's answer is the mean of the values it sees: whatever a score's
+    rounding is it is the same for all, 2^-11 for the weights, 2^-19 for sums and half a step of the output are left."""
+    p = prompt(np.random.default_rng(46), path, "f16", 700)
+    m = p.c.model["k"]
+    m.codes[:], m.scale[:] = 64, np.float32(2.0 ** -6)
+    p.put("k")
+    m = p.c.model["v"]
+    m.scale[:] = np.float32(2.0 ** -6)
+    p.put("v")
+    p.q, p.values[:] = torch.ones_like(p.q), 1.0
+    out = attend(p, path, at / math.log2(math.e) / DIM).double().cpu().numpy()
+    v = p.c.model["v"].rows(p.c.table[0], 700)[0]
+    for r in np.arange(p.new)[::-37]:
+        n = p.sees(r)
+        want, spread = v[:, :n].mean(1), np.abs(v[:, :n]).mean(1)
+        allowed = spread * (2.0 ** -11 + 2.0 ** -19) + np.abs(want) * 2.0 ** -11 * 1.01 + 2.0 ** -25
+        assert (np.abs(out[r] - want) <= allowed).all(), r
