@@ -278,7 +278,8 @@ typedef struct {
 } pq_paged_config;
 
 /* As pq_attn_validate_config, pq_attn_codes_bytes, pq_attn_create and pq_attn_destroy: the bytes are those of
- * k_cache, or of v_cache. */
+ * k_cache, or of v_cache.  A context is destroyed after the graphs that recorded its calls (they use its scratch), and not
+ * while a graph is recorded. */
 int pq_paged_validate_config(const pq_paged_config *cfg /* host */);
 int64_t pq_paged_cache_bytes(const pq_paged_config *cfg /* host */);
 int pq_paged_create(const pq_paged_config *cfg /* host */, pq_paged_ctx **out /* host */);
@@ -349,7 +350,8 @@ int pq_paged_decode(pq_paged_ctx *ctx, int32_t n_seqs, const void *q, int64_t q_
  * seq_len[b] - tok_len[b] + i + 1 tokens (a row for which that is not positive gets zeros).
  *
  *   n_tokens             rows of q and out, >= the end of the last sequence's rows (the kernels are chosen by what they are
- *                        on average: a call padded to many times its tokens is right, but slower)
+ *                        on average: a call padded to many times its tokens is right, but slower, and so is one that
+ *                        has long prompts and requests of few tokens over very long caches: give those a call of their own)
  *   q                    as in pq_paged_decode, row t at t * q_stride elements
  *   seq_len              lengths after the step (pq_paged_plan's new_seq_len)
  *   tok_start, tok_len   device int32, as pq_paged_plan gives them (rows from n_tokens on are left out, a sequence whose

@@ -413,7 +413,8 @@ def pq_paged_device_error(ctx) -> int:
 
 
 class PQPaged:
-    """A context of pq_paged_create, destroyed with the object; `handle` is what the pq_paged_* calls take."""
+    """A context of pq_paged_create, destroyed with the object; `handle` is what the pq_paged_* calls take.  Keep the object as
+    long as any graph that recorded such a call."""
 
     handle: Optional[int] = None
 

@@ -7,10 +7,12 @@
 // scores came in (V's tokens lie in LDS in the order in which the result of the first product holds them).  A lane has one query
 // row: its maximum, sum, limit and rescaling are its own.
 //
-// Bound by the issue of matrix and vector instructions, which two wavefronts of a SIMD overlap only in part: a prompt of 8K tokens,
-// 32 query / 8 KV heads of 128 dims in bf16, takes 594 us (925 TFLOP/s; matrix units busy 41 % of the time, vector units 48 %).
+// Bound by the issue of matrix and vector instructions, which two wavefronts of a SIMD overlap only in part, and by waits: a
+// prompt of 8K tokens, 32 query / 8 KV heads of 128 dims in bf16, takes 580 to 590 us (932 to 948 TFLOP/s; matrix units busy 42 % of
+// the time, vector units 50 %, 40 % of the wavefronts' cycles are waits), in fp32, with operands in two parts, 963 us.
 // Without its exponentials it would take 20 us less, without the conversion of bytes 61, without the search for the maximum
-// 50, without the second product 156: no one of them stands out.
+// 50, without the second product 156: no one of them stands out.  (Sums of weights before their rounding instead of after: no
+// change, 580 and 583 us.  The way for scores beyond 2^22 costs the others 0.3 %.)
 #include <hip/hip_runtime.h>
 
 #include "pq_paged_work.h"
