@@ -16,7 +16,7 @@
 
 // how pq_paged_decode's workgroups are cut out, and what they exchange through
 struct pq_paged_decode_plan {
-    float *partials;        // [head group][2 budget slots][sub_rows][d + 2]: maximum, sum, sums of values
+    float *partials;        // [head group][2 budget slots][sub_rows][d + 2]: base, sum, sums of values
     unsigned int *tickets;  // one per slot, zero between calls
     int n_sub, sub_rows;    // head groups of a KV head, and query heads of one (the last may have fewer)
     int budget;             // chunks per head group that a call's tokens are cut into
@@ -24,7 +24,7 @@ struct pq_paged_decode_plan {
 
 // How pq_paged_prefill shares out a call: sequences of at most few_rows rows (tokens times query heads of a KV head) in tiles of
 // PQ_PAGED_FEW_ROWS, whose keys are cut into about `budget` pieces per KV head (0: not cut), the others in tiles of
-// PQ_PAGED_TILE_ROWS.  Partials: for each KV head [2 budget slots][PQ_PAGED_FEW_ROWS][d + 2]: maximum, sum, sums of values.
+// PQ_PAGED_TILE_ROWS.  Partials: for each KV head [2 budget slots][PQ_PAGED_FEW_ROWS][d + 2]: base, sum, sums of values.
 #define PQ_PAGED_TILE_ROWS 256
 #define PQ_PAGED_FEW_ROWS 32
 struct pq_paged_prefill_plan {

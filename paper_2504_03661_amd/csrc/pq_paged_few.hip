@@ -291,7 +291,7 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void pq_paged_merge_kernel(pq_pag
         const float *from = w.partials + ((int64_t)h * (2 * w.budget) + p.slot) * stride + r * (D + 2);
         float top = LOWEST, sum = 0.0f, x = 0.0f, y = 0.0f;
         for (int c0 = 0; c0 < tile.pieces; c0 += 64, from += 64 * stride) {
-            // a lane has a piece's maximum and sum, and so its weight; one that is not there has the weight 0
+            // a lane has a piece's base and sum, and so its weight; one that is not there has the weight 0
             const int n = tile.pieces - c0 < 64 ? tile.pieces - c0 : 64;
             const float2 ml = lane < n ? *(const float2 *)(from + lane * stride) : make_float2(-INFINITY, 0.0f);
             const float high = fmaxf(top, wave_max(ml.x)), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
