@@ -241,8 +241,8 @@ int pq_attn_device_error(pq_attn_ctx *ctx, uint32_t *flags /* host */);
  *
  * Blocks.  n_blocks blocks of block_tokens tokens.  Sequence b holds block_table[b][0 .. ceil(len / block_tokens) - 1];
  * its token at position p is in slot block_table[b][p / block_tokens] * block_tokens + p % block_tokens.  Requests may
- * name the same blocks (a shared prefix) as long as none of them appends to a shared one and the program keeps count of
- * the holders: pq_paged_plan gives back all blocks of a request that ends.
+ * name the same blocks (a shared prefix) as long as none of them appends to a shared one and the holders are counted:
+ * pq_paged_plan gives back all blocks of a request that ends.  pq_paged_fork, pq_paged_free and pq_paged_compact keep that count.
  *
  * Values.  With x the values of one KV head's tokens in a block (K and V each for itself):
  *     scale = max(max |x|, 127 * 2^-40) / 127, rounded to fp32;  code = x / scale, rounded to the nearest integer, ties
@@ -366,8 +366,104 @@ int pq_paged_prefill(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const 
                      const int32_t *block_table, const int32_t *seq_len, const int32_t *tok_start, const int32_t *tok_len,
                      float scale, void *out, void *hip_stream);
 
-/* As pq_attn_device_error.  Bit 0: pq_paged_plan refused a request; bit 1: a block number or slot outside the cache; bit 2: the
- * sequences of a pq_paged_prefill claimed more rows than it had. */
+/* Requests that hold blocks together.  holders[x] is the number of requests that hold block x besides the first: an array
+ * of n_blocks int32 that the program sets to zero once, that pq_paged_fork, pq_paged_free and pq_paged_compact keep (never
+ * negative between calls; a program that keeps blocks by itself, for prompts that may come again, adds and takes away 1 likewise), and
+ * that pq_paged_plan need not know: a block that it gives or takes has 0.  Requests end by pq_paged_free then: pq_paged_plan with the
+ * same n_new behind it finds them empty and gives back nothing twice.
+ *
+ * Requests that begin as copies of others: samples of one prompt, beams, chats with the same first part.
+ *
+ *   parent       device [n_seqs] int32  request whose tokens request b begins with; negative, or b: request b stays as it is
+ *   keep         device [n_seqs] int32  tokens it takes of them at most (negative: none); NULL: all
+ *   seq_len      device [n_seqs] int32  tokens cached now; a request that becomes a fork has 0
+ *   free_list, free_count, block_table  as in pq_paged_plan (the list is only read)
+ *   holders      device [n_blocks] int32, changed in place
+ *   new_seq_len, new_free_count         after the call (may be the same arrays as seq_len, free_count)
+ *   copy_src/dst device [n_seqs] int32  the block whose contents request b needs in a block of its own; -1 where it needs none
+ *
+ * With n = min(seq_len[parent[b]], keep[b]) request b holds the first n / block_tokens blocks of its parent with it.  Where n is not a
+ * multiple of block_tokens it takes a free block from the top of the stack, in the order of the requests, and copy_src[b], copy_dst[b]
+ * say what is to be copied, in the caches of every layer (pq_paged_copy), before anything is appended.  All
+ * lengths are those before the call: a fork of a request that is itself empty is empty.  A request that is not empty, whose
+ * parent is not one of the n_seqs, or that finds no block free for it and all that have asked before it stays as it
+ * is, and bit 0 of the device error word is set. */
+int pq_paged_fork(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *parent, const int32_t *keep, const int32_t *seq_len,
+                  const int32_t *free_list, const int32_t *free_count, int32_t *block_table, int32_t *holders,
+                  int32_t *new_seq_len, int32_t *new_free_count, int32_t *copy_src, int32_t *copy_dst, void *hip_stream);
+
+/* Requests that end: each takes 1 from the holders of its blocks, and those that have no holder left go onto the stack of free
+ * blocks, from the highest number down (the lowest is taken first).
+ *
+ *   n_new        device [n_seqs] int32  negative: request b ends, as for pq_paged_plan; the others stay as they are
+ *   the others   as in pq_paged_fork; free_list is changed in place, block_table only read
+ *
+ * A block that more requests give back than hold it goes back once, and bit 3 of the device error word is set. */
+int pq_paged_free(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *n_new, const int32_t *seq_len, int32_t *free_list,
+                  const int32_t *free_count, const int32_t *block_table, int32_t *holders, int32_t *new_seq_len,
+                  int32_t *new_free_count, void *hip_stream);
+
+/* Live blocks (those that are not on the stack of free ones) moved together, so that with n_live of them no number from
+ * n_live on is in use: a cache of n_live blocks or more can take their place, and what is free lies in a row.  The k-th highest
+ * live block at or behind n_live goes to the k-th lowest free number in front of it; the others stay.
+ *
+ *   n_seqs                    all requests that hold blocks
+ *   seq_len, block_table, holders, free_list, free_count  as in pq_paged_fork
+ *   new_block_table, new_holders, new_free_list, new_free_count  after the call (may be the same arrays as the former).  Table
+ *                             entries behind a request's blocks, and list entries behind the count, are left as they were; the
+ *                             list is n_blocks - 1, n_blocks - 2, .., n_live
+ *   moved_to      device [n_blocks] int32  each block's new number (for what else names blocks); -1 for a free one
+ *   copy_src/dst  device [n_blocks] int32, n_copies device [1] int32  the blocks that move, and how many: for pq_paged_copy in the
+ *                             caches of every layer, before anything else reads or writes them by the new numbers.  Entries
+ *                             behind n_copies are left as they were
+ *
+ * A block that is on the list twice counts once.  A table's entry that is on the list, or outside the cache, sets bit 1 of the
+ * device error word; the former becomes -1. */
+int pq_paged_compact(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *seq_len, const int32_t *free_list,
+                     const int32_t *free_count, const int32_t *block_table, const int32_t *holders, int32_t *new_free_list,
+                     int32_t *new_free_count, int32_t *new_block_table, int32_t *new_holders, int32_t *moved_to,
+                     int32_t *copy_src, int32_t *copy_dst, int32_t *n_copies, void *hip_stream);
+
+/* Contents and scales of blocks src[i] of one cache into blocks dst[i] of another, or of the same: a fork's, a compacted cache's, or
+ * requests on their way to a cache elsewhere and back (host memory that the device can address will do).
+ *
+ *   n_pairs       entries of src and dst (device int32), 0 ..; 0 does nothing.  A pair with a negative src is passed over
+ *   count         device [1] int32  pairs to be looked at, if fewer; NULL: all
+ *   n_from, n_to  blocks of the two caches, which have this context's heads, dims and block_tokens (n * block_tokens < 2^31,
+ *                 PQ_ERR_CAPACITY otherwise).  A number outside sets bit 1 of the device error word, and its pair copies nothing
+ *
+ * A block that comes twice in dst holds parts of either source; one that is in dst and, of the same cache, in src of another pair leaves
+ * that pair's block unspecified (pq_paged_fork and pq_paged_compact give no such pairs). */
+int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const int32_t *dst, const int32_t *count,
+                  int32_t n_from, const uint8_t *from_k, const uint8_t *from_v, const float *from_k_scale,
+                  const float *from_v_scale, int32_t n_to, uint8_t *to_k, uint8_t *to_v, float *to_k_scale,
+                  float *to_v_scale, void *hip_stream);
+
+/* pq_paged_decode for groups of requests that begin with the same blocks: those are read once for a group.
+ *
+ *   n_groups     1 .. n_seqs (PQ_ERR_SHAPE, PQ_ERR_CAPACITY otherwise)
+ *   members      device [n_seqs] int32  requests, group after group, each at most once; NULL: 0, 1, .., n_seqs - 1
+ *   group_start  device [n_groups + 1] int32  group g is members[group_start[g]] .. members[group_start[g + 1] - 1] (not
+ *                ascending: a group that would begin before the one in front of it begins where that does)
+ *   shared_len   device [n_groups] int32  tokens that all members of a group begin with, in the same blocks.  What counts is whole
+ *                blocks, and no more than the first member has: they are read by its block table.  A member that is shorter attends over
+ *                its own length of them
+ *   workspace    device, 16-byte aligned, at least pq_paged_shared_workspace_bytes(ctx, n_seqs, n_groups) bytes (else
+ *                PQ_ERR_CAPACITY); contents need not be initialised.  Calls that may run at the same time need one each
+ *   out          device [n_seqs][Hq][d] dtype; rows of requests that are in no group are left as they were
+ *
+ * The others as in pq_paged_decode, and so is the result; a number in members that is no request sets bit 1 of the device error
+ * word.  pq_paged_shared_workspace_bytes returns a negative pq_status for sizes that the call would refuse. */
+int64_t pq_paged_shared_workspace_bytes(const pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups);
+int pq_paged_shared_decode(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups, const void *q, int64_t q_stride,
+                           const uint8_t *k_cache, const uint8_t *v_cache, const float *k_scale, const float *v_scale,
+                           const int32_t *block_table, const int32_t *seq_len, const int32_t *members,
+                           const int32_t *group_start, const int32_t *shared_len, float scale, void *workspace,
+                           int64_t workspace_bytes, void *out, void *hip_stream);
+
+/* As pq_attn_device_error.  Bit 0: pq_paged_plan or pq_paged_fork refused a request; bit 1: a block number, slot or request outside
+ * the cache or the call; bit 2: the sequences of a pq_paged_prefill claimed more rows than it had; bit 3: pq_paged_free gave a block back
+ * more often than it was held. */
 int pq_paged_device_error(pq_paged_ctx *ctx, uint32_t *flags /* host */);
 
 /* Static, never NULL. */

@@ -52,6 +52,104 @@ def plan(n_new, seq_len, free_list, free_count, table, block, n_tokens):
             "refused": refused}
 
 
+# ------------------------------------------------------------------------------------------------ blocks held together
+
+def _lengths(seq_len, table, block):
+    return [min(max(int(n), 0), table.shape[1] * block) for n in seq_len]
+
+
+def fork(parent, keep, seq_len, free_list, free_count, table, holders, block):
+    """pq_paged_fork, request after request.  Nothing given is changed.  Returns a dict of its outputs, and what it reports."""
+    table, holders, free = np.array(table), np.array(holders), list(map(int, free_list))
+    n_blocks, old, before = len(free), _lengths(seq_len, table, block), np.array(table)
+    count = min(max(int(free_count), 0), n_blocks)
+    top, asked = count, 0
+    length, src, dst, refused, outside = list(old), [], [], False, False
+    for b, p in enumerate(map(int, parent)):
+        pair = (-1, -1)
+        if p >= 0 and p != b:
+            if p >= len(old) or old[b] != 0:
+                refused = True
+            else:
+                n = old[p] if keep is None else max(0, min(old[p], int(keep[b])))
+                full, last = n // block, int(before[p, n // block]) if n % block else -1
+                needs = n % block != 0 and 0 <= last < n_blocks
+                asked += needs
+                if needs and asked > count:
+                    refused = True
+                else:
+                    for j in range(full):
+                        x = table[b, j] = before[p, j]
+                        if 0 <= x < n_blocks:
+                            holders[x] += 1
+                        else:
+                            outside = True
+                    if needs:
+                        top -= 1
+                        pair = (last, free[top])
+                        table[b, full] = free[top]
+                    elif n % block:
+                        table[b, full], outside = last, True
+                    length[b] = n
+        src.append(pair[0])
+        dst.append(pair[1])
+    return {"new_seq_len": np.array(length), "new_free_count": np.array([top]), "block_table": table, "holders": holders,
+            "copy_src": np.array(src), "copy_dst": np.array(dst), "refused": refused, "outside": outside}
+
+
+def free(n_new, seq_len, free_list, free_count, table, holders, block):
+    """pq_paged_free.  Nothing given is changed."""
+    table, left, listed = np.array(table), np.array(holders, np.int64), np.array(free_list)
+    n_blocks, old = len(listed), _lengths(seq_len, np.array(table), block)
+    gone, over, outside = set(), False, False
+    for b, n in enumerate(n_new):
+        for x in map(int, table[b, :-(-old[b] // block)] if n < 0 else []):
+            if not 0 <= x < n_blocks:
+                outside = True
+            elif x in gone:
+                over = True
+            elif left[x] > 0:
+                left[x] -= 1
+            else:
+                gone.add(x)
+    count = min(max(int(free_count), 0), n_blocks)
+    for x in sorted(gone, reverse=True):
+        if count < n_blocks:
+            listed[count] = x
+            count += 1
+    return {"new_seq_len": np.array([0 if n < 0 else m for n, m in zip(n_new, old)]), "new_free_count": np.array([count]),
+            "free_list": listed, "holders": left, "over": over, "outside": outside}
+
+
+def compact(seq_len, free_list, free_count, table, holders, block):
+    """pq_paged_compact.  Lists hold only what the call writes of them."""
+    table, holders = np.array(table), np.array(holders)
+    n_blocks, old = len(holders), _lengths(seq_len, table, block)
+    listed = [int(x) for x in free_list[:min(max(int(free_count), 0), n_blocks)]]
+    gone = {x for x in listed if 0 <= x < n_blocks}
+    outside = len(gone) < len(set(listed))
+    n_live = n_blocks - len(gone)
+    src = [x for x in range(n_blocks - 1, n_live - 1, -1) if x not in gone]
+    dst = [x for x in range(n_live) if x in gone]
+    assert len(src) == len(dst)
+    moved = {x: -1 if x in gone else x for x in range(n_blocks)} | dict(zip(src, dst))
+    new_holders = np.zeros_like(holders)
+    for x, to in moved.items():
+        if to >= 0:
+            new_holders[to] = holders[x]
+    for b, n in enumerate(old):
+        for j in range(-(-n // block)):
+            x = int(table[b, j])
+            if 0 <= x < n_blocks:
+                table[b, j] = moved[x]
+                outside |= moved[x] < 0
+            else:
+                outside = True
+    return {"new_free_list": np.arange(n_blocks - 1, n_live - 1, -1), "new_free_count": np.array([len(gone)]),
+            "new_block_table": table, "new_holders": new_holders, "moved_to": np.array([moved[x] for x in range(n_blocks)]),
+            "copy_src": np.array(src, int), "copy_dst": np.array(dst, int), "n_copies": np.array([len(src)]), "outside": outside}
+
+
 # ------------------------------------------------------------------------------------------------------------ cache
 
 def nearest(x, s):

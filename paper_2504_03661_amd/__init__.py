@@ -6,4 +6,5 @@ from .binding import (  # noqa: F401
     pq_stream_read_probe, pq_unpack_codes,
     PQPaged, PQPagedConfig, pq_paged_append, pq_paged_cache_bytes, pq_paged_create, pq_paged_decode, pq_paged_destroy,
     pq_paged_device_error, pq_paged_plan, pq_paged_prefill, pq_paged_read, pq_paged_validate_config,
+    pq_paged_compact, pq_paged_copy, pq_paged_fork, pq_paged_free, pq_paged_shared_decode, pq_paged_shared_workspace_bytes,
 )

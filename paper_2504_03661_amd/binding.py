@@ -155,6 +155,18 @@ def load_library():
     L.pq_paged_decode.argtypes = [vp, i32, vp, i64] + [vp] * 6 + [f32, vp, vp]
     L.pq_paged_prefill.restype = ctypes.c_int
     L.pq_paged_prefill.argtypes = [vp, i32, i32, vp, i64] + [vp] * 8 + [f32, vp, vp]
+    L.pq_paged_fork.restype = ctypes.c_int
+    L.pq_paged_fork.argtypes = [vp, i32] + [vp] * 12
+    L.pq_paged_free.restype = ctypes.c_int
+    L.pq_paged_free.argtypes = [vp, i32] + [vp] * 9
+    L.pq_paged_compact.restype = ctypes.c_int
+    L.pq_paged_compact.argtypes = [vp, i32] + [vp] * 14
+    L.pq_paged_copy.restype = ctypes.c_int
+    L.pq_paged_copy.argtypes = [vp, i32, vp, vp, vp, i32] + [vp] * 4 + [i32] + [vp] * 5
+    L.pq_paged_shared_workspace_bytes.restype = i64
+    L.pq_paged_shared_workspace_bytes.argtypes = [vp, i32, i32]
+    L.pq_paged_shared_decode.restype = ctypes.c_int
+    L.pq_paged_shared_decode.argtypes = [vp, i32, i32, vp, i64] + [vp] * 9 + [f32, vp, i64, vp, vp]
     L.pq_paged_device_error.restype = ctypes.c_int
     L.pq_paged_device_error.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
     L.pq_status_string.restype = ctypes.c_char_p
@@ -162,7 +174,7 @@ def load_library():
     _calls = calls
     _decode_at = ctypes.cast(L.pq_attn_decode, vp).value
     _append_at = ctypes.cast(L.pq_encode_append, vp).value
-    for name in ("plan", "append", "read", "decode", "prefill"):
+    for name in ("plan", "append", "read", "decode", "prefill", "fork", "free", "compact", "copy", "shared_decode"):
         _paged_at[name] = ctypes.cast(getattr(L, "pq_paged_" + name), vp).value
     _lib = L
     return L
@@ -404,6 +416,90 @@ def pq_paged_prefill(ctx, n_seqs, n_tokens, q, q_stride, k_cache, v_cache, k_sca
                                 _addr(tok_start), _addr(tok_len), float(scale), _addr(out), _stream(stream))
     if rc:
         raise PQAttnError(rc, "pq_paged_prefill")
+
+
+def pq_paged_fork(ctx, n_seqs, parent, keep, seq_len, free_list, free_count, block_table, holders, new_seq_len,
+                  new_free_count, copy_src, copy_dst, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_fork(_paged_at["fork"], _current_stream, ctx, n_seqs, parent, keep, seq_len, free_list,
+                               free_count, block_table, holders, new_seq_len, new_free_count, copy_src, copy_dst,
+                               stream)
+    else:
+        rc = L.pq_paged_fork(ctx, int(n_seqs), _addr(parent), _addr(keep), _addr(seq_len), _addr(free_list),
+                             _addr(free_count), _addr(block_table), _addr(holders), _addr(new_seq_len),
+                             _addr(new_free_count), _addr(copy_src), _addr(copy_dst), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_fork")
+
+
+def pq_paged_free(ctx, n_seqs, n_new, seq_len, free_list, free_count, block_table, holders, new_seq_len,
+                  new_free_count, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_free(_paged_at["free"], _current_stream, ctx, n_seqs, n_new, seq_len, free_list, free_count,
+                               block_table, holders, new_seq_len, new_free_count, stream)
+    else:
+        rc = L.pq_paged_free(ctx, int(n_seqs), _addr(n_new), _addr(seq_len), _addr(free_list), _addr(free_count),
+                             _addr(block_table), _addr(holders), _addr(new_seq_len), _addr(new_free_count),
+                             _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_free")
+
+
+def pq_paged_compact(ctx, n_seqs, seq_len, free_list, free_count, block_table, holders, new_free_list, new_free_count,
+                     new_block_table, new_holders, moved_to, copy_src, copy_dst, n_copies, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_compact(_paged_at["compact"], _current_stream, ctx, n_seqs, seq_len, free_list, free_count,
+                                  block_table, holders, new_free_list, new_free_count, new_block_table, new_holders,
+                                  moved_to, copy_src, copy_dst, n_copies, stream)
+    else:
+        rc = L.pq_paged_compact(ctx, int(n_seqs), _addr(seq_len), _addr(free_list), _addr(free_count),
+                                _addr(block_table), _addr(holders), _addr(new_free_list), _addr(new_free_count),
+                                _addr(new_block_table), _addr(new_holders), _addr(moved_to), _addr(copy_src),
+                                _addr(copy_dst), _addr(n_copies), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_compact")
+
+
+def pq_paged_copy(ctx, n_pairs, src, dst, count, n_from, from_k, from_v, from_k_scale, from_v_scale, n_to, to_k, to_v,
+                  to_k_scale, to_v_scale, stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_copy(_paged_at["copy"], _current_stream, ctx, n_pairs, src, dst, count, n_from, from_k,
+                               from_v, from_k_scale, from_v_scale, n_to, to_k, to_v, to_k_scale, to_v_scale, stream)
+    else:
+        rc = L.pq_paged_copy(ctx, int(n_pairs), _addr(src), _addr(dst), _addr(count), int(n_from), _addr(from_k),
+                             _addr(from_v), _addr(from_k_scale), _addr(from_v_scale), int(n_to), _addr(to_k),
+                             _addr(to_v), _addr(to_k_scale), _addr(to_v_scale), _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_copy")
+
+
+def pq_paged_shared_workspace_bytes(ctx, n_seqs, n_groups) -> int:
+    n = int(load_library().pq_paged_shared_workspace_bytes(ctx, int(n_seqs), int(n_groups)))
+    if n < 0:
+        raise PQAttnError(n, "pq_paged_shared_workspace_bytes")
+    return n
+
+
+def pq_paged_shared_decode(ctx, n_seqs, n_groups, q, q_stride, k_cache, v_cache, k_scale, v_scale, block_table,
+                           seq_len, members, group_start, shared_len, scale, workspace, workspace_bytes, out,
+                           stream=None) -> None:
+    L = _lib or load_library()
+    if _calls is not None and isinstance(ctx, _CONTEXT):
+        rc = _calls.paged_shared_decode(_paged_at["shared_decode"], _current_stream, ctx, n_seqs, n_groups, q,
+                                        q_stride, k_cache, v_cache, k_scale, v_scale, block_table, seq_len, members,
+                                        group_start, shared_len, scale, workspace, workspace_bytes, out, stream)
+    else:
+        rc = L.pq_paged_shared_decode(ctx, int(n_seqs), int(n_groups), _addr(q), int(q_stride), _addr(k_cache),
+                                      _addr(v_cache), _addr(k_scale), _addr(v_scale), _addr(block_table),
+                                      _addr(seq_len), _addr(members), _addr(group_start), _addr(shared_len),
+                                      float(scale), _addr(workspace), int(workspace_bytes), _addr(out),
+                                      _stream(stream))
+    if rc:
+        raise PQAttnError(rc, "pq_paged_shared_decode")
 
 
 def pq_paged_device_error(ctx) -> int:

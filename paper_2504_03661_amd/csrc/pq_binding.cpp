@@ -130,9 +130,9 @@ PyObject *append(PyObject *, PyObject *const *a, Py_ssize_t n)
     return PyLong_FromLong(rc);
 }
 
-// The five calls of the paged cache: their arguments by kind, in the order of pq_attn.h (h context, p pointer, i int32, l int64,
+// The calls of the paged cache: their arguments by kind, in the order of pq_attn.h (h context, p pointer, i int32, l int64,
 // f float; the stream comes last).
-constexpr int MOST = 16;
+constexpr int MOST = 20;
 
 union argument {
     void *p;
@@ -201,10 +201,26 @@ PAGED_CALL(paged_decode, "hiplppppppfp", (P, int32_t, P, int64_t, P, P, P, P, P,
 PAGED_CALL(paged_prefill, "hiiplppppppppfp", (P, int32_t, int32_t, P, int64_t, P, P, P, P, P, P, P, P, float, P, P),
            (a[0].p, a[1].i, a[2].i, a[3].p, a[4].l, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p, a[13].f,
             a[14].p, a[15].p))
+PAGED_CALL(paged_fork, "hippppppppppp", (P, int32_t, P, P, P, P, P, P, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p,
+            a[13].p))
+PAGED_CALL(paged_free, "hipppppppp", (P, int32_t, P, P, P, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p))
+PAGED_CALL(paged_compact, "hippppppppppppp", (P, int32_t, P, P, P, P, P, P, P, P, P, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p,
+            a[13].p, a[14].p, a[15].p))
+PAGED_CALL(paged_copy, "hipppippppipppp", (P, int32_t, P, P, P, int32_t, P, P, P, P, int32_t, P, P, P, P, P),
+           (a[0].p, a[1].i, a[2].p, a[3].p, a[4].p, a[5].i, a[6].p, a[7].p, a[8].p, a[9].p, a[10].i, a[11].p, a[12].p,
+            a[13].p, a[14].p, a[15].p))
+PAGED_CALL(paged_shared_decode, "hiiplpppppppppfplp", (P, int32_t, int32_t, P, int64_t, P, P, P, P, P, P, P, P, P, float, P,
+                                                       int64_t, P, P),
+           (a[0].p, a[1].i, a[2].i, a[3].p, a[4].l, a[5].p, a[6].p, a[7].p, a[8].p, a[9].p, a[10].p, a[11].p, a[12].p,
+            a[13].p, a[14].f, a[15].p, a[16].l, a[17].p, a[18].p))
 
 #define METHOD(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(decode), METHOD(append), METHOD(paged_plan), METHOD(paged_append), METHOD(paged_read),
-                         METHOD(paged_decode), METHOD(paged_prefill), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(paged_decode), METHOD(paged_prefill), METHOD(paged_fork), METHOD(paged_free),
+                         METHOD(paged_compact), METHOD(paged_copy), METHOD(paged_shared_decode), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pq_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -13,6 +13,7 @@
 #define PQ_PAGED_ERRFLAG_REFUSED 1u
 #define PQ_PAGED_ERRFLAG_RANGE 2u
 #define PQ_PAGED_ERRFLAG_CLAIMS 4u
+#define PQ_PAGED_ERRFLAG_HOLDERS 8u
 
 // how pq_paged_decode's workgroups are cut out, and what they exchange through
 struct pq_paged_decode_plan {
@@ -39,7 +40,7 @@ struct pq_paged_ctx {
     char *scratch;          // the allocation that the pointers below and in the plans point into
     pq_paged_decode_plan decode;
     pq_paged_prefill_plan prefill;
-    int *plan;              // scratch of pq_paged_plan: what its two launches hand over
+    int *plan;              // what the launches of pq_paged_plan, fork, free and compact hand over
     unsigned int *dev_err;  // sticky error word
 };
 
@@ -80,6 +81,44 @@ struct pq_paged_read_args {
     int n_seqs, n_rows;
 };
 
+struct pq_paged_fork_args {
+    const int32_t *parent, *keep;  // keep: or NULL
+    const int32_t *seq_len, *free_list, *free_count;
+    int32_t *table, *holders, *new_seq_len, *new_free_count, *copy_src, *copy_dst;
+    int *scratch;
+    int n_seqs, n_blocks, max_blocks, log_block;
+    unsigned int *dev_err;
+};
+
+struct pq_paged_free_args {
+    const int32_t *n_new, *seq_len;
+    int32_t *free_list;
+    const int32_t *free_count, *table;
+    int32_t *holders, *new_seq_len, *new_free_count;
+    int *scratch;
+    int n_seqs, n_blocks, max_blocks, log_block;
+    unsigned int *dev_err;
+};
+
+struct pq_paged_compact_args {
+    const int32_t *seq_len, *free_list, *free_count, *table, *holders;
+    int32_t *new_free_list, *new_free_count, *new_table, *new_holders, *moved_to, *copy_src, *copy_dst, *n_copies;
+    int *scratch;
+    int n_seqs, n_blocks, max_blocks, log_block;
+    unsigned int *dev_err;
+};
+
+struct pq_paged_copy_args {
+    const int32_t *src, *dst, *count;  // count: or NULL
+    const uint8_t *from[2];
+    const float *from_scale[2];
+    uint8_t *to[2];
+    float *to_scale[2];
+    int64_t block_bytes;  // of K, and of V
+    int n_pairs, n_from, n_to, Hkv;
+    unsigned int *dev_err;
+};
+
 struct pq_paged_attn_args {
     pq_paged_view c;
     const void *q;
@@ -94,6 +133,11 @@ int64_t pq_paged_plan_scratch_bytes();
 hipError_t pq_launch_paged_plan(const pq_paged_ctx *ctx, const pq_paged_plan_args &a, hipStream_t s);
 hipError_t pq_launch_paged_append(const pq_paged_ctx *ctx, const pq_paged_append_args &a, hipStream_t s);
 hipError_t pq_launch_paged_read(const pq_paged_ctx *ctx, const pq_paged_read_args &a, hipStream_t s);
+int64_t pq_paged_blocks_scratch_bytes();
+hipError_t pq_launch_paged_fork(const pq_paged_fork_args &a, hipStream_t s);
+hipError_t pq_launch_paged_free(const pq_paged_free_args &a, hipStream_t s);
+hipError_t pq_launch_paged_compact(const pq_paged_compact_args &a, hipStream_t s);
+hipError_t pq_launch_paged_copy(const pq_paged_copy_args &a, int n_cu, hipStream_t s);
 pq_paged_decode_plan pq_paged_plan_decode(const pq_paged_config *cfg, int n_cu);
 int64_t pq_paged_decode_slots(const pq_paged_config *cfg, const pq_paged_decode_plan &w);
 int64_t pq_paged_decode_slot_floats(const pq_paged_config *cfg, const pq_paged_decode_plan &w);

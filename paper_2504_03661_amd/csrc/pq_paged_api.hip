@@ -6,6 +6,7 @@
 #include <new>
 
 #include "pq_paged.h"
+#include "pq_paged_shared.h"
 
 namespace {
 
@@ -56,6 +57,19 @@ int check_tokens(const pq_paged_ctx *ctx, int32_t n_tokens)
     return n_tokens < 0 ? PQ_ERR_SHAPE : n_tokens > ctx->cfg.max_tokens ? PQ_ERR_CAPACITY : PQ_OK;
 }
 
+int check_groups(const pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups)
+{
+    const int rc = check_seqs(ctx, n_seqs);
+    return rc != PQ_OK ? rc : n_groups < 1 ? PQ_ERR_SHAPE : n_groups > n_seqs ? PQ_ERR_CAPACITY : PQ_OK;
+}
+
+int check_attention(const pq_paged_ctx *ctx, const void *q, int64_t q_stride, const uint8_t *k, const uint8_t *v, float scale, const void *out)
+{
+    if (!aligned(q) || !aligned(out) || !aligned(k) || !aligned(v) || !stride_fits(ctx, q_stride, ctx->cfg.n_q_heads))
+        return PQ_ERR_SHAPE;
+    return fabsf(scale * LOG2E) <= FLT_MAX ? PQ_OK : PQ_ERR_SHAPE;  // NaN or infinite, or so in what the kernels multiply by
+}
+
 pq_paged_view view(const pq_paged_ctx *ctx, const uint8_t *k, const uint8_t *v, const float *k_scale, const float *v_scale,
                    const int32_t *table, const int32_t *seq_len)
 {
@@ -83,10 +97,9 @@ void free_ctx(pq_paged_ctx *ctx)
 int attend(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const void *q, int64_t q_stride, const pq_paged_view &c,
            const int32_t *tok_start, const int32_t *tok_len, float scale, void *out, void *hip_stream)
 {
-    if (!aligned(q) || !aligned(out) || !aligned(c.k) || !aligned(c.v) || !stride_fits(ctx, q_stride, ctx->cfg.n_q_heads))
-        return PQ_ERR_SHAPE;
-    if (!(fabsf(scale * LOG2E) <= FLT_MAX))  // NaN or infinite, or so in what the kernels multiply by
-        return PQ_ERR_SHAPE;
+    const int rc = check_attention(ctx, q, q_stride, c.k, c.v, scale, out);
+    if (rc != PQ_OK)
+        return rc;
     device_guard guard(ctx->cfg.device);
     if (!guard.ok)
         return PQ_ERR_HIP;
@@ -153,7 +166,8 @@ int pq_paged_create(const pq_paged_config *cfg, pq_paged_ctx **out)
     const auto room = [&](size_t n) { const size_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
     const size_t err_at = room(sizeof(unsigned int)), tickets_at = room(slots * sizeof(unsigned int));
     const size_t zeros = bytes;
-    const size_t plan_at = room((size_t)pq_paged_plan_scratch_bytes());
+    const int64_t of_plan = pq_paged_plan_scratch_bytes(), of_blocks = pq_paged_blocks_scratch_bytes();
+    const size_t plan_at = room((size_t)(of_plan > of_blocks ? of_plan : of_blocks));
     const size_t decode_at = room((size_t)slots * pq_paged_decode_slot_floats(cfg, ctx->decode) * sizeof(float));
     const size_t prefill_at = room((size_t)pq_paged_prefill_floats(cfg, ctx->prefill) * sizeof(float));
     if (hipMalloc((void **)&ctx->scratch, bytes) != hipSuccess) {
@@ -319,6 +333,196 @@ int pq_paged_prefill(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_tokens, const 
         return PQ_OK;
     return attend(ctx, n_seqs, n_tokens, q, q_stride, view(ctx, k_cache, v_cache, k_scale, v_scale, block_table, seq_len),
                   tok_start, tok_len, scale, out, hip_stream);
+}
+
+int pq_paged_fork(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *parent, const int32_t *keep, const int32_t *seq_len,
+                  const int32_t *free_list, const int32_t *free_count, int32_t *block_table, int32_t *holders,
+                  int32_t *new_seq_len, int32_t *new_free_count, int32_t *copy_src, int32_t *copy_dst, void *hip_stream)
+{
+    if (ctx == nullptr || parent == nullptr || seq_len == nullptr || free_list == nullptr || free_count == nullptr ||
+        block_table == nullptr || holders == nullptr || new_seq_len == nullptr || new_free_count == nullptr ||
+        copy_src == nullptr || copy_dst == nullptr)
+        return PQ_ERR_NULL;
+    const int rc = check_seqs(ctx, n_seqs);
+    if (rc != PQ_OK)
+        return rc;
+    device_guard guard(ctx->cfg.device);
+    if (!guard.ok)
+        return PQ_ERR_HIP;
+    pq_paged_fork_args a;
+    a.parent = parent;
+    a.keep = keep;
+    a.seq_len = seq_len;
+    a.free_list = free_list;
+    a.free_count = free_count;
+    a.table = block_table;
+    a.holders = holders;
+    a.new_seq_len = new_seq_len;
+    a.new_free_count = new_free_count;
+    a.copy_src = copy_src;
+    a.copy_dst = copy_dst;
+    a.scratch = ctx->plan;
+    a.n_seqs = n_seqs;
+    a.n_blocks = ctx->cfg.n_blocks;
+    a.max_blocks = ctx->cfg.max_blocks;
+    a.log_block = ctx->log_block;
+    a.dev_err = ctx->dev_err;
+    return pq_launch_paged_fork(a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
+}
+
+int pq_paged_free(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *n_new, const int32_t *seq_len, int32_t *free_list,
+                  const int32_t *free_count, const int32_t *block_table, int32_t *holders, int32_t *new_seq_len,
+                  int32_t *new_free_count, void *hip_stream)
+{
+    if (ctx == nullptr || n_new == nullptr || seq_len == nullptr || free_list == nullptr || free_count == nullptr ||
+        block_table == nullptr || holders == nullptr || new_seq_len == nullptr || new_free_count == nullptr)
+        return PQ_ERR_NULL;
+    const int rc = check_seqs(ctx, n_seqs);
+    if (rc != PQ_OK)
+        return rc;
+    device_guard guard(ctx->cfg.device);
+    if (!guard.ok)
+        return PQ_ERR_HIP;
+    pq_paged_free_args a;
+    a.n_new = n_new;
+    a.seq_len = seq_len;
+    a.free_list = free_list;
+    a.free_count = free_count;
+    a.table = block_table;
+    a.holders = holders;
+    a.new_seq_len = new_seq_len;
+    a.new_free_count = new_free_count;
+    a.scratch = ctx->plan;
+    a.n_seqs = n_seqs;
+    a.n_blocks = ctx->cfg.n_blocks;
+    a.max_blocks = ctx->cfg.max_blocks;
+    a.log_block = ctx->log_block;
+    a.dev_err = ctx->dev_err;
+    return pq_launch_paged_free(a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
+}
+
+int pq_paged_compact(pq_paged_ctx *ctx, int32_t n_seqs, const int32_t *seq_len, const int32_t *free_list,
+                     const int32_t *free_count, const int32_t *block_table, const int32_t *holders, int32_t *new_free_list,
+                     int32_t *new_free_count, int32_t *new_block_table, int32_t *new_holders, int32_t *moved_to,
+                     int32_t *copy_src, int32_t *copy_dst, int32_t *n_copies, void *hip_stream)
+{
+    if (ctx == nullptr || seq_len == nullptr || free_list == nullptr || free_count == nullptr || block_table == nullptr ||
+        holders == nullptr || new_free_list == nullptr || new_free_count == nullptr || new_block_table == nullptr ||
+        new_holders == nullptr || moved_to == nullptr || copy_src == nullptr || copy_dst == nullptr || n_copies == nullptr)
+        return PQ_ERR_NULL;
+    const int rc = check_seqs(ctx, n_seqs);
+    if (rc != PQ_OK)
+        return rc;
+    device_guard guard(ctx->cfg.device);
+    if (!guard.ok)
+        return PQ_ERR_HIP;
+    pq_paged_compact_args a;
+    a.seq_len = seq_len;
+    a.free_list = free_list;
+    a.free_count = free_count;
+    a.table = block_table;
+    a.holders = holders;
+    a.new_free_list = new_free_list;
+    a.new_free_count = new_free_count;
+    a.new_table = new_block_table;
+    a.new_holders = new_holders;
+    a.moved_to = moved_to;
+    a.copy_src = copy_src;
+    a.copy_dst = copy_dst;
+    a.n_copies = n_copies;
+    a.scratch = ctx->plan;
+    a.n_seqs = n_seqs;
+    a.n_blocks = ctx->cfg.n_blocks;
+    a.max_blocks = ctx->cfg.max_blocks;
+    a.log_block = ctx->log_block;
+    a.dev_err = ctx->dev_err;
+    return pq_launch_paged_compact(a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
+}
+
+int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const int32_t *dst, const int32_t *count,
+                  int32_t n_from, const uint8_t *from_k, const uint8_t *from_v, const float *from_k_scale,
+                  const float *from_v_scale, int32_t n_to, uint8_t *to_k, uint8_t *to_v, float *to_k_scale,
+                  float *to_v_scale, void *hip_stream)
+{
+    if (ctx == nullptr || from_k == nullptr || from_v == nullptr || from_k_scale == nullptr || from_v_scale == nullptr ||
+        to_k == nullptr || to_v == nullptr || to_k_scale == nullptr || to_v_scale == nullptr ||
+        (n_pairs != 0 && (src == nullptr || dst == nullptr)))
+        return PQ_ERR_NULL;
+    if (n_pairs < 0 || n_from < 1 || n_to < 1 || !aligned(from_k) || !aligned(from_v) || !aligned(to_k) || !aligned(to_v))
+        return PQ_ERR_SHAPE;
+    if (n_pairs > INT32_MAX / ctx->cfg.block_tokens || n_from > INT32_MAX / ctx->cfg.block_tokens ||
+        n_to > INT32_MAX / ctx->cfg.block_tokens)
+        return PQ_ERR_CAPACITY;
+    if (n_pairs == 0)
+        return PQ_OK;
+    device_guard guard(ctx->cfg.device);
+    if (!guard.ok)
+        return PQ_ERR_HIP;
+    pq_paged_copy_args a;
+    a.src = src;
+    a.dst = dst;
+    a.count = count;
+    a.from[0] = from_k;
+    a.from[1] = from_v;
+    a.from_scale[0] = from_k_scale;
+    a.from_scale[1] = from_v_scale;
+    a.to[0] = to_k;
+    a.to[1] = to_v;
+    a.to_scale[0] = to_k_scale;
+    a.to_scale[1] = to_v_scale;
+    a.block_bytes = (int64_t)ctx->cfg.n_kv_heads * ctx->cfg.block_tokens * ctx->cfg.head_dim;
+    a.n_pairs = n_pairs;
+    a.n_from = n_from;
+    a.n_to = n_to;
+    a.Hkv = ctx->cfg.n_kv_heads;
+    a.dev_err = ctx->dev_err;
+    return pq_launch_paged_copy(a, ctx->n_cu, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
+}
+
+int64_t pq_paged_shared_workspace_bytes(const pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups)
+{
+    if (ctx == nullptr)
+        return PQ_ERR_NULL;
+    const int rc = check_groups(ctx, n_seqs, n_groups);
+    return rc != PQ_OK ? rc : pq_paged_shared_layout(ctx, n_seqs, n_groups, nullptr, nullptr);
+}
+
+int pq_paged_shared_decode(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups, const void *q, int64_t q_stride,
+                           const uint8_t *k_cache, const uint8_t *v_cache, const float *k_scale, const float *v_scale,
+                           const int32_t *block_table, const int32_t *seq_len, const int32_t *members,
+                           const int32_t *group_start, const int32_t *shared_len, float scale, void *workspace,
+                           int64_t workspace_bytes, void *out, void *hip_stream)
+{
+    if (ctx == nullptr || q == nullptr || k_cache == nullptr || v_cache == nullptr || k_scale == nullptr ||
+        v_scale == nullptr || block_table == nullptr || seq_len == nullptr || group_start == nullptr ||
+        shared_len == nullptr || workspace == nullptr || out == nullptr)
+        return PQ_ERR_NULL;
+    int rc = check_groups(ctx, n_seqs, n_groups);
+    rc = rc == PQ_OK ? check_attention(ctx, q, q_stride, k_cache, v_cache, scale, out) : rc;
+    if (rc != PQ_OK)
+        return rc;
+    if (!aligned(workspace))
+        return PQ_ERR_SHAPE;
+    pq_paged_shared_args a;
+    if (workspace_bytes < pq_paged_shared_layout(ctx, n_seqs, n_groups, workspace, &a.w))
+        return PQ_ERR_CAPACITY;
+    device_guard guard(ctx->cfg.device);
+    if (!guard.ok)
+        return PQ_ERR_HIP;
+    a.c = view(ctx, k_cache, v_cache, k_scale, v_scale, block_table, seq_len);
+    a.q = q;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.members = members;
+    a.group_start = group_start;
+    a.shared_len = shared_len;
+    a.scale_log2e = scale * LOG2E;
+    a.n_seqs = n_seqs;
+    a.n_groups = n_groups;
+    a.Hq = ctx->cfg.n_q_heads;
+    a.G = ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads;
+    a.budget = pq_paged_shared_budget(ctx);
+    return pq_launch_paged_shared(ctx, a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
 }
 
 int pq_paged_device_error(pq_paged_ctx *ctx, uint32_t *flags)

@@ -1,0 +1,385 @@
+// pq_paged_fork, pq_paged_free, pq_paged_compact and pq_paged_copy: blocks that requests hold together.
+//
+// holders[x] is the number of requests that hold block x besides the first, so that a block that one request holds, and a free
+// one, need no entry of their own: 0 is what pq_paged_plan finds and leaves.  A fork adds 1 for every block it shares; an end takes 1
+// away, and the one that finds 0 leaves -1 behind: the block has no holder.  Sums of integers, so the order of the atomics
+// does not matter; one that finds less than 0 takes its step back, and a block goes back once whatever the counts were.
+//
+// What goes onto the stack of free blocks is put in order by its number, not by who gave it: that is the same in every run, and
+// the lowest numbers, on top, are taken first.
+#include <hip/hip_runtime.h>
+
+#include "pq_paged_scan.h"
+
+namespace {
+
+constexpr int SEGMENTS = 256;  // of the block numbers, at most, each a workgroup's
+constexpr int ROW_THREADS = 256;
+
+// what a call's launches hand over, in the context's scratch
+struct blocks_scratch {
+    int shares[PQ_PAGED_MAX_SEQS];  // fork: blocks that a row shares with its parent
+    int count[SEGMENTS];            // free, compact: of each segment
+    int free_count;                 // free: before the call
+    int n_live;                     // compact
+};
+
+__device__ inline bool in_range(int x, int n) { return (unsigned)x < (unsigned)n; }
+
+__device__ inline int length_of(const int32_t *seq_len, int b, int most) { return between(seq_len[b], most); }
+
+// ---------------------------------------------------------------------------------------------------------- fork
+
+// Who becomes whose fork, and the block that it needs for itself: one workgroup, a chunk of 1024 rows at a time.
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fork_args a)
+{
+    __shared__ int length[PQ_PAGED_MAX_SEQS];
+    __shared__ scan_room room;
+    blocks_scratch &s = *(blocks_scratch *)a.scratch;
+    const int most = a.max_blocks << a.log_block, round = (1 << a.log_block) - 1;
+    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS)
+        length[b] = length_of(a.seq_len, b, most);
+    const int count = between(a.free_count[0], a.n_blocks);
+    __syncthreads();
+    int before = 0;  // blocks asked for by the rows of the chunks before
+    bool refused = false, range = false;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += SCAN_THREADS) {
+        const int b = b0 + threadIdx.x;
+        int n = 0, last = -1, p = -1;
+        bool asks = false, fits = false;
+        if (b < a.n_seqs) {
+            p = a.parent[b];
+            asks = p >= 0 && p != b;
+            fits = asks && p < a.n_seqs && length[b] == 0;
+            if (fits) {
+                n = length[p];
+                if (a.keep != nullptr)
+                    n = between(a.keep[b], n);
+                if ((n & round) != 0)
+                    last = a.table[(int64_t)p * a.max_blocks + (n >> a.log_block)];
+            }
+        }
+        const bool part = (n & round) != 0, needs = part && in_range(last, a.n_blocks);
+        int upto = needs, unused = 0, all, all_unused;
+        scan_two(upto, unused, room, all, all_unused);
+        upto += before;
+        before += all;
+        if (b < a.n_seqs) {
+            const bool granted = fits && (!needs || upto <= count);
+            const int got = needs && granted ? a.free_list[count - upto] : -1;
+            a.copy_src[b] = needs && granted ? last : -1;
+            a.copy_dst[b] = got;
+            a.new_seq_len[b] = granted ? n : length[b];
+            s.shares[b] = granted ? n >> a.log_block : 0;
+            if (granted && part)  // (a number outside the cache stays what it is: nobody follows it)
+                a.table[(int64_t)b * a.max_blocks + (n >> a.log_block)] = needs ? got : last;
+            refused |= asks && !granted;
+            range |= granted && part && !needs;
+        }
+    }
+    if (threadIdx.x == 0)
+        a.new_free_count[0] = count - at_most(before, count);
+    if (refused)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_REFUSED);
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+}
+
+// The shared blocks into the rows' tables, and counted.  A row that gets blocks was empty: nobody reads it.
+__global__ __launch_bounds__(ROW_THREADS) void pq_paged_fork_tables_kernel(pq_paged_fork_args a)
+{
+    const blocks_scratch &s = *(const blocks_scratch *)a.scratch;
+    const int b = blockIdx.x, n = s.shares[b];
+    if (n == 0)
+        return;
+    const int32_t *from = a.table + (int64_t)a.parent[b] * a.max_blocks;
+    int32_t *to = a.table + (int64_t)b * a.max_blocks;
+    bool range = false;
+    for (int j = blockIdx.y * ROW_THREADS + threadIdx.x; j < n; j += gridDim.y * ROW_THREADS) {
+        const int x = from[j];
+        to[j] = x;
+        if (in_range(x, a.n_blocks))
+            atomicAdd(a.holders + x, 1);
+        else
+            range = true;
+    }
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+}
+
+// ---------------------------------------------------------------------------------------------------------- free
+
+__global__ __launch_bounds__(ROW_THREADS) void pq_paged_release_kernel(pq_paged_free_args a)
+{
+    const int b = blockIdx.x;
+    if (a.n_new[b] >= 0)
+        return;
+    const int n = length_of(a.seq_len, b, a.max_blocks << a.log_block), used = (n + (1 << a.log_block) - 1) >> a.log_block;
+    const int32_t *row = a.table + (int64_t)b * a.max_blocks;
+    bool range = false, over = false;
+    for (int j = blockIdx.y * ROW_THREADS + threadIdx.x; j < used; j += gridDim.y * ROW_THREADS) {
+        const int x = row[j];
+        if (!in_range(x, a.n_blocks)) {
+            range = true;
+        } else if (atomicSub(a.holders + x, 1) < 0) {
+            atomicAdd(a.holders + x, 1);
+            over = true;
+        }
+    }
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+    if (over)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_HOLDERS);
+}
+
+// How many numbers of a segment are negative: blocks without a holder (free), free blocks (compact).
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_count_kernel(const int32_t *x, int n, int per_segment, int *scratch, const int32_t *free_count)
+{
+    __shared__ scan_room room;
+    blocks_scratch &s = *(blocks_scratch *)scratch;
+    const int first = blockIdx.x * per_segment, end = n - first < per_segment ? n : first + per_segment;
+    int found = 0, unused = 0, all, all_unused;
+    for (int i = first + threadIdx.x; i < end; i += SCAN_THREADS)
+        found += x[i] < 0;
+    scan_two(found, unused, room, all, all_unused);
+    if (threadIdx.x == 0) {
+        s.count[blockIdx.x] = all;
+        if (blockIdx.x == 0 && free_count != nullptr)
+            s.free_count = between(free_count[0], n);
+    }
+}
+
+// Sums of the segments before this workgroup's and of all.
+__device__ inline void segment_sums(const blocks_scratch &s, int n_segments, scan_room &room, int &before, int &all)
+{
+    const int t = threadIdx.x, mine = t < n_segments ? s.count[t] : 0;
+    int x = mine, y = t < (int)blockIdx.x ? mine : 0, all_x, all_y;
+    scan_two(x, y, room, all_x, all_y);
+    before = all_y;
+    all = all_x;
+}
+
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_push_kernel(pq_paged_free_args a, int per_segment)
+{
+    __shared__ scan_room room;
+    const blocks_scratch &s = *(const blocks_scratch *)a.scratch;
+    int below, all;
+    segment_sums(s, gridDim.x, room, below, all);
+    const int first = blockIdx.x * per_segment, end = a.n_blocks - first < per_segment ? a.n_blocks : first + per_segment;
+    int place = s.free_count + all - below - s.count[blockIdx.x];  // of the segment's highest block
+    for (int e = end; e > first; e -= SCAN_THREADS) {
+        const int x = e - 1 - (int)threadIdx.x;
+        const bool goes = x >= first && a.holders[x] < 0;
+        int upto = goes, unused = 0, found, all_unused;
+        scan_two(upto, unused, room, found, all_unused);
+        if (goes) {
+            a.holders[x] = 0;
+            if (place + upto - 1 < a.n_blocks)
+                a.free_list[place + upto - 1] = x;
+        }
+        place += found;
+    }
+    for (int b = blockIdx.x * SCAN_THREADS + threadIdx.x; b < a.n_seqs; b += gridDim.x * SCAN_THREADS)
+        a.new_seq_len[b] = a.n_new[b] < 0 ? 0 : length_of(a.seq_len, b, a.max_blocks << a.log_block);
+    if (blockIdx.x == 0 && threadIdx.x == 0)
+        a.new_free_count[0] = at_most(s.free_count + all, a.n_blocks);
+}
+
+// ---------------------------------------------------------------------------------------------------------- compact
+
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_mark_kernel(pq_paged_compact_args a, bool clear)
+{
+    const int first = blockIdx.x * SCAN_THREADS + threadIdx.x, step = gridDim.x * SCAN_THREADS;
+    if (clear) {
+        for (int i = first; i < a.n_blocks; i += step)
+            a.moved_to[i] = 0;
+        return;
+    }
+    const int count = between(a.free_count[0], a.n_blocks);
+    bool range = false;
+    for (int i = first; i < count; i += step) {
+        const int x = a.free_list[i];
+        if (in_range(x, a.n_blocks))
+            a.moved_to[x] = -1;
+        else
+            range = true;
+    }
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+}
+
+// The k-th highest live block at or behind n_live goes to the k-th lowest free number in front of it.  moved_to becomes the
+// block's number where it stays, -1 where it is free, -2 - k where it moves.
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_pair_kernel(pq_paged_compact_args a, int per_segment)
+{
+    __shared__ scan_room room;
+    blocks_scratch &s = *(blocks_scratch *)a.scratch;
+    int below, n_free;  // free numbers below this chunk's, and all
+    segment_sums(s, gridDim.x, room, below, n_free);
+    const int n_live = a.n_blocks - n_free;
+    const int first = blockIdx.x * per_segment, end = a.n_blocks - first < per_segment ? a.n_blocks : first + per_segment;
+    for (int i0 = first; i0 < end; i0 += SCAN_THREADS) {
+        const int i = i0 + threadIdx.x;
+        const bool there = i < end, is_free = there && a.moved_to[i] < 0;
+        int upto = is_free, unused = 0, found, all_unused;
+        scan_two(upto, unused, room, found, all_unused);
+        upto += below;  // free numbers up to i
+        below += found;
+        if (!there)
+            continue;
+        if (i == n_live)
+            a.n_copies[0] = upto - is_free;
+        if (is_free) {
+            if (i < n_live)
+                a.copy_dst[upto - 1] = i;
+        } else if (i < n_live) {
+            a.moved_to[i] = i;
+        } else {
+            const int k = (a.n_blocks - 1 - i) - (n_free - upto);  // live blocks above it
+            a.copy_src[k] = i;
+            a.moved_to[i] = -2 - k;
+        }
+    }
+    for (int i = blockIdx.x * SCAN_THREADS + threadIdx.x; i < n_free; i += gridDim.x * SCAN_THREADS)
+        a.new_free_list[i] = a.n_blocks - 1 - i;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        a.new_free_count[0] = n_free;
+        s.n_live = n_live;
+        if (n_free == 0)
+            a.n_copies[0] = 0;
+    }
+}
+
+// Tables and counts by the new numbers.  A number that is read while moved_to gets its last values is one or the other,
+// which say the same.
+__global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged_compact_args a, int row_groups)
+{
+    const blocks_scratch &s = *(const blocks_scratch *)a.scratch;
+    const auto moved = [&](int x) {
+        const int v = __hip_atomic_load(a.moved_to + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        return v < -1 ? a.copy_dst[-2 - v] : v;
+    };
+    if ((int)blockIdx.x < a.n_seqs * row_groups) {
+        const int b = blockIdx.x / row_groups, group = blockIdx.x - b * row_groups;
+        const int n = length_of(a.seq_len, b, a.max_blocks << a.log_block), used = (n + (1 << a.log_block) - 1) >> a.log_block;
+        bool range = false;
+        for (int j = group * ROW_THREADS + threadIdx.x; j < used; j += row_groups * ROW_THREADS) {
+            const int64_t at = (int64_t)b * a.max_blocks + j;
+            const int x = a.table[at];
+            const int to = in_range(x, a.n_blocks) ? moved(x) : x;
+            a.new_table[at] = to;
+            range |= to < 0 || !in_range(x, a.n_blocks);
+        }
+        if (range)
+            paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+        return;
+    }
+    const int groups = gridDim.x - a.n_seqs * row_groups;
+    for (int i = (blockIdx.x - a.n_seqs * row_groups) * ROW_THREADS + threadIdx.x; i < a.n_blocks; i += groups * ROW_THREADS) {
+        const int v = a.moved_to[i];
+        if (i < s.n_live) {
+            if (v >= 0)  // (a free one gets its count from the block that moves there)
+                a.new_holders[i] = a.holders[i];
+        } else {
+            if (v < -1) {
+                const int to = a.copy_dst[-2 - v];
+                a.new_holders[to] = a.holders[i];
+                __hip_atomic_store(a.moved_to + i, to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            a.new_holders[i] = 0;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------- copy
+
+constexpr int COPY_THREADS = 256;
+constexpr int COPY_LOADS = 4;  // 16-byte loads of a thread on their way together
+constexpr int COPY_UNIT = COPY_THREADS * COPY_LOADS * 16;
+
+__global__ __launch_bounds__(COPY_THREADS) void pq_paged_copy_kernel(pq_paged_copy_args a)
+{
+    const int count = a.count == nullptr ? a.n_pairs : between(a.count[0], a.n_pairs);
+    const int parts = (int)((a.block_bytes + COPY_UNIT - 1) / COPY_UNIT);
+    const int64_t units = (int64_t)count * 2 * parts;
+    bool range = false;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int pair = (int)(u / (2 * parts)), rest = (int)(u - (int64_t)pair * (2 * parts)), kind = rest / parts, part = rest - kind * parts;
+        const int src = a.src[pair], dst = a.dst[pair];
+        if (src < 0)
+            continue;
+        if (src >= a.n_from || !in_range(dst, a.n_to)) {
+            range = true;
+            continue;
+        }
+        const uint8_t *from = a.from[kind] + src * a.block_bytes;
+        uint8_t *to = a.to[kind] + dst * a.block_bytes;
+        const int64_t at = (int64_t)part * COPY_UNIT + threadIdx.x * 16;
+        u32x4 x[COPY_LOADS];
+#pragma unroll
+        for (int i = 0; i < COPY_LOADS; ++i)
+            if (at + i * (COPY_THREADS * 16) < a.block_bytes)
+                x[i] = *(const u32x4 *)(from + at + i * (COPY_THREADS * 16));
+#pragma unroll
+        for (int i = 0; i < COPY_LOADS; ++i)
+            if (at + i * (COPY_THREADS * 16) < a.block_bytes)
+                *(u32x4 *)(to + at + i * (COPY_THREADS * 16)) = x[i];
+        if (part == 0)
+            for (int h = threadIdx.x; h < a.Hkv; h += COPY_THREADS)
+                a.to_scale[kind][(int64_t)dst * a.Hkv + h] = a.from_scale[kind][(int64_t)src * a.Hkv + h];
+    }
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+}
+
+// blocks of a segment: a multiple of what a workgroup takes at a time
+int per_segment(int n_blocks) { return (n_blocks / SEGMENTS / SCAN_THREADS + 1) * SCAN_THREADS; }
+int segments(int n_blocks) { return (n_blocks + per_segment(n_blocks) - 1) / per_segment(n_blocks); }
+
+// workgroups of a table's row: four entries a thread where it is that long
+int groups_of_row(int max_blocks)
+{
+    const int n = (max_blocks + 4 * ROW_THREADS - 1) / (4 * ROW_THREADS);
+    return n < 16 ? n : 16;
+}
+
+}  // namespace
+
+int64_t pq_paged_blocks_scratch_bytes() { return sizeof(blocks_scratch); }
+
+hipError_t pq_launch_paged_fork(const pq_paged_fork_args &a, hipStream_t s)
+{
+    hipLaunchKernelGGL(pq_paged_fork_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
+    hipLaunchKernelGGL(pq_paged_fork_tables_kernel, dim3(a.n_seqs, groups_of_row(a.max_blocks)), dim3(ROW_THREADS), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t pq_launch_paged_free(const pq_paged_free_args &a, hipStream_t s)
+{
+    hipLaunchKernelGGL(pq_paged_release_kernel, dim3(a.n_seqs, groups_of_row(a.max_blocks)), dim3(ROW_THREADS), 0, s, a);
+    const int n = segments(a.n_blocks), per = per_segment(a.n_blocks);
+    hipLaunchKernelGGL(pq_paged_count_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a.holders, a.n_blocks, per, a.scratch, a.free_count);
+    hipLaunchKernelGGL(pq_paged_push_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a, per);
+    return hipGetLastError();
+}
+
+hipError_t pq_launch_paged_compact(const pq_paged_compact_args &a, hipStream_t s)
+{
+    const int n = segments(a.n_blocks), per = per_segment(a.n_blocks);
+    const int marks = (a.n_blocks + SCAN_THREADS - 1) / SCAN_THREADS;
+    const dim3 grid(marks < 512 ? marks : 512);
+    hipLaunchKernelGGL(pq_paged_mark_kernel, grid, dim3(SCAN_THREADS), 0, s, a, true);
+    hipLaunchKernelGGL(pq_paged_mark_kernel, grid, dim3(SCAN_THREADS), 0, s, a, false);
+    hipLaunchKernelGGL(pq_paged_count_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a.moved_to, a.n_blocks, per, a.scratch, (const int32_t *)nullptr);
+    hipLaunchKernelGGL(pq_paged_pair_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a, per);
+    const int rows = groups_of_row(a.max_blocks), others = (a.n_blocks + ROW_THREADS - 1) / ROW_THREADS;
+    hipLaunchKernelGGL(pq_paged_renumber_kernel, dim3(a.n_seqs * rows + (others < 1024 ? others : 1024)), dim3(ROW_THREADS), 0, s, a, rows);
+    return hipGetLastError();
+}
+
+hipError_t pq_launch_paged_copy(const pq_paged_copy_args &a, int n_cu, hipStream_t s)
+{
+    const int64_t units = (int64_t)a.n_pairs * 2 * ((a.block_bytes + COPY_UNIT - 1) / COPY_UNIT), most = 8 * n_cu;
+    hipLaunchKernelGGL(pq_paged_copy_kernel, dim3((unsigned)(units < most ? units : most)), dim3(COPY_THREADS), 0, s, a);
+    return hipGetLastError();
+}

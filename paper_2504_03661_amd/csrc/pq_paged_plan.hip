@@ -13,12 +13,12 @@
 // in memory and the entries one kind after another; 1000 requests with 114K tokens: 13.2 us).
 #include <hip/hip_runtime.h>
 
-#include "pq_paged_tile.h"
+#include "pq_paged_scan.h"
 
 namespace {
 
-constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_WAVES = PLAN_THREADS / 64;
+constexpr int PLAN_THREADS = SCAN_THREADS;
+constexpr int PLAN_WAVES = SCAN_WAVES;
 
 // the numbers of every request, and behind the last one their sums
 struct plan_sums {
@@ -29,39 +29,6 @@ struct plan_sums {
     int got[PQ_PAGED_MAX_SEQS];        // tokens that have a place
     int count, there;                  // free blocks before the call, and after the pushes
 };
-
-struct scan_room {
-    int wave[2][PLAN_WAVES];
-};
-
-// Inclusive sums over the workgroup's threads of two numbers, and their totals.
-__device__ inline void scan_two(int &x, int &y, scan_room &room, int &all_x, int &all_y)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    x = lane_scan(x);
-    y = lane_scan(y);
-    if (lane == 63) {
-        room.wave[0][wave] = x;
-        room.wave[1][wave] = y;
-    }
-    __syncthreads();
-    int before_x = 0, before_y = 0;
-    all_x = all_y = 0;
-#pragma unroll
-    for (int w = 0; w < PLAN_WAVES; ++w) {
-        const int of_x = room.wave[0][w], of_y = room.wave[1][w];
-        before_x += w < wave ? of_x : 0;
-        before_y += w < wave ? of_y : 0;
-        all_x += of_x;
-        all_y += of_y;
-    }
-    __syncthreads();
-    x += before_x;
-    y += before_y;
-}
-
-__device__ inline int between(int n, int most) { return n < 0 ? 0 : n > most ? most : n; }
-__device__ inline int at_most(int x, int most) { return x > most ? most : x; }
 
 // The first half.  All sums are kept in 32 bits: what a request adds is limited to 2^20 + 1 (more rows than a call can have, all
 // blocks of a sequence), a chunk of 1024 to 2^30, and the sums behind a chunk to what still decides the same.
@@ -148,20 +115,6 @@ __device__ void plan_requests(const pq_paged_plan_args &a, plan_sums &s, scan_ro
     if (refused)
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_REFUSED);
     __syncthreads();
-}
-
-// the last i of [0, n) with sums[i] <= x, for x >= sums[0] = 0
-__device__ inline int owner(const int *sums, int n, int x)
-{
-    int low = 0, high = n;
-    while (high - low > 1) {
-        const int mid = (low + high) >> 1;
-        if (sums[mid] <= x)
-            low = mid;
-        else
-            high = mid;
-    }
-    return low;
 }
 
 // The i-th block that this call takes: it lies i below the top, among those pushed by this call or below them.

@@ -1,0 +1,306 @@
+"""pq_paged_shared_decode against the plain model in 64 bits, within bounds derived in paged_inputs.bound."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2504_03661_amd as pq
+from oracle import paged_oracle as O
+from tests.paged_inputs import TORCH, check, context, dev
+from tests.test_gpu_paged_attn import queries
+
+pytestmark = pytest.mark.gpu
+
+
+class Groups:
+    """A cache of random codes and scales, and requests that hold the first blocks of their group's prompt together.  groups:
+    for each (shared tokens, [length of each member]).  Blocks that nobody holds have NaN scales: whoever reads one shows it."""
+
+    def __init__(self, rng, groups, Hkv, dim, block, spare=3, order=True):
+        self.groups, self.block, self.dim = groups, block, dim
+        lengths = np.array([n for _, members in groups for n in members], int)
+        self.seqs = len(lengths)
+        rows = rng.permutation(self.seqs) if order else np.arange(self.seqs)
+        self.start = np.concatenate([[0], np.cumsum([len(m) for _, m in groups])])
+        used = -(-lengths // block)
+        self.width = int(max(1, used.max(initial=1)))
+        numbers = iter(rng.permutation(int(used.sum()) + sum(s // block for s, _ in groups) + spare))
+        table, held = np.full((self.seqs, self.width), -1), set()
+        for g, (shared, members) in enumerate(groups):
+            prompt = [next(numbers) for _ in range(shared // block)]
+            for i in range(self.start[g], self.start[g + 1]):
+                n = min(len(prompt), used[i])
+                table[rows[i], :n] = prompt[:n]
+                table[rows[i], n:used[i]] = [next(numbers) for _ in range(used[i] - n)]
+                held |= set(table[rows[i], :used[i]].tolist())
+        self.n_blocks = int(used.sum()) + sum(s // block for s, _ in groups) + spare
+        self.table, self.members, self.lengths = table, rows, np.zeros(self.seqs, int)
+        self.lengths[rows] = lengths
+        self.data, self.scale, self.model = {}, {}, {}
+        nobody = [x for x in range(self.n_blocks) if x not in held]
+        for kind in "kv":
+            scale = np.exp2(rng.uniform(-7.0, -5.0, (self.n_blocks, Hkv))).astype(np.float32)
+            scale[nobody] = np.nan
+            data = rng.integers(1, 256, (self.n_blocks, Hkv, block * dim), dtype=np.uint8)
+            self.model[kind] = O.Cache.from_bytes(data, scale, block, dim, kind == "v")
+            self.data[kind], self.scale[kind] = dev(data, torch.uint8), dev(scale, torch.float32)
+        self.device_members, self.device_start = dev(rows), dev(self.start)
+        self.shared, self.seq_len, self.block_table = dev([s for s, _ in groups]), dev(self.lengths), dev(table)
+
+    def context(self, dtype, Hq, Hkv):
+        return context(dtype, Hq, Hkv, self.dim, self.block, self.n_blocks, self.width, self.seqs)
+
+    def cache(self):
+        return self.data["k"], self.data["v"], self.scale["k"], self.scale["v"], self.block_table, self.seq_len
+
+    def call(self, ctx, q, out, scale, workspace=None, members=True):
+        workspace = work(ctx, self.seqs, len(self.groups)) if workspace is None else workspace
+        pq.pq_paged_shared_decode(ctx.handle, self.seqs, len(self.groups), q, q.shape[1], *self.cache(),
+                                  self.device_members if members else None, self.device_start, self.shared, scale, workspace,
+                                  workspace.numel(), out)
+        return out
+
+    def expected(self, values, scale):
+        parts = []
+        for b in range(self.seqs):
+            n = int(self.lengths[b])
+            (k, there), (v, _) = (self.model[kind].rows(self.table[b], n) for kind in "kv")
+            parts.append(O.attention(values[b:b + 1], k, v, there, scale, [n]))
+        return [np.concatenate(x) for x in zip(*parts)]
+
+
+def work(ctx, seqs, groups):
+    """A workspace of just the bytes that are asked for, full of NaN."""
+    n = pq.pq_paged_shared_workspace_bytes(ctx.handle, seqs, groups)
+    return torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+
+
+def empty(c, Hq, dtype, fill=float("nan")):
+    return torch.full((c.seqs, Hq, c.dim), fill, dtype=TORCH[dtype], device="cuda")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (4, 4), (8, 2), (7, 1), (32, 8), (28, 4), (16, 1), (33, 1), (40, 1)])
+def test_heads_and_types(dtype, Hq, Hkv):
+    rng = np.random.default_rng(Hq * 100 + Hkv)
+    for dim, block in ((128, 16), (64, 32)):
+        c = Groups(rng, [(64, [64, 100, 301]), (0, [37]), (192, [192, 193]), (32, [0, 32, 1])], Hkv, dim, block)
+        ctx = c.context(dtype, Hq, Hkv)
+        q, values = queries(rng, c.seqs, Hq, dim, dtype, gap=8 * (Hq % 3))
+        scale = 1.0 / math.sqrt(dim)
+        out = c.call(ctx, q, empty(c, Hq, dtype), scale)
+        check(out, *c.expected(values, scale), dtype, dim, f"{dim}")
+        assert pq.pq_paged_device_error(ctx.handle) == 0
+
+
+@pytest.mark.parametrize("dtype,block,dim", [("f16", 16, 128), ("bf16", 64, 128), ("f32", 32, 64), ("f16", 32, 64)])
+def test_lengths_around_every_border(dtype, block, dim):
+    """Shared lengths and lengths behind them at which a block, a step, a wavefront's share or a piece may end."""
+    rng = np.random.default_rng(block)
+    groups = []
+    for shared in (block, 2 * block, 3 * block, 128, 192, 256, 320, 512, 576, 1024):
+        groups.append((shared, [shared + e for e in rng.choice([0, 1, 15, 16, 17, 31, 32, 33, 127, 128, 129, 255, 256, 257, 500], 5)]))
+    c = Groups(rng, groups, 2, dim, block)
+    ctx = c.context(dtype, 6, 2)
+    q, values = queries(rng, c.seqs, 6, dim, dtype)
+    out = c.call(ctx, q, empty(c, 6, dtype), 0.11)
+    check(out, *c.expected(values, 0.11), dtype, dim)
+
+
+@pytest.mark.parametrize("groups", [
+    [(9008, [9008 + 7 * i for i in range(9)])],
+    [(20000, [20000, 20001]), (16, [20, 3000]), (0, [0, 17, 5])],
+    [(1024, [1024 + i for i in range(70)])],
+    [(48, [48 + 3 * i for i in range(n)]) for n in range(1, 12)],
+    [(0, [700] * 3), (640, [640, 9000, 640, 641])],
+])
+def test_long_prompts_and_many_members(groups):
+    rng = np.random.default_rng(len(groups))
+    for dtype, Hq, Hkv in (("f16", 4, 4), ("bf16", 8, 1), ("f32", 4, 2)):
+        c = Groups(rng, groups, Hkv, 128, 16)
+        ctx = c.context(dtype, Hq, Hkv)
+        q, values = queries(rng, c.seqs, Hq, 128, dtype)
+        want = c.expected(values, 0.09)
+        first = None
+        for again in range(3):
+            out = c.call(ctx, q, empty(c, Hq, dtype), 0.09)
+            check(out, *want, dtype, 128, f"{dtype} call {again}")
+            first = out if first is None else first
+            assert torch.equal(out, first)                    # bit for bit
+
+
+def test_members_in_order_and_shorter_than_what_is_shared():
+    """members NULL; shared_len that is no whole number of blocks, more than the first member has, negative, more than others have."""
+    rng = np.random.default_rng(20)
+    c = Groups(rng, [(160, [200, 161, 170]), (320, [320, 320, 400]), (64, [64, 500]), (96, [300, 96, 10, 0])], 2, 128, 16, order=False)
+    c.lengths[1], c.lengths[2] = 40, 0                        # their tables keep all the blocks
+    c.seq_len.copy_(dev(c.lengths))
+    c.shared.copy_(dev([175, 10 ** 9, -5, 97]))
+    c.lengths[3] = 330
+    c.seq_len.copy_(dev(c.lengths))
+    c.table[3, 20] = c.table[5, 20]
+    c.block_table.copy_(dev(np.clip(c.table, -1, None)))
+    ctx = c.context("f16", 8, 2)
+    q, values = queries(rng, c.seqs, 8, 128, "f16")
+    out = c.call(ctx, q, empty(c, 8, "f16"), 0.1, members=False)
+    check(out, *c.expected(values, 0.1), "f16", 128)
+    assert pq.pq_paged_device_error(ctx.handle) == 0
+
+
+def test_rows_of_no_group_stay_as_they_were():
+    """Positions in front of the first group and behind the last, numbers that are no request, groups that are not ascending."""
+    rng = np.random.default_rng(21)
+    c = Groups(rng, [(64, [70, 80, 90, 100, 110, 120, 130, 140])], 1, 64, 16, order=False)
+    c.groups = [0, 1, 2, 3]
+    ctx = c.context("f16", 4, 1)
+    q, values = queries(rng, 8, 4, 64, "f16")
+    want = c.expected(values, 0.1)
+    for start, members, inside, told in (([1, 3, 3, 5, 6], [0, 1, 2, 3, 4, 5, 6, 7], [1, 2, 3, 4, 5], 0),
+                                         ([0, 4, 2, 6, 6], [7, 6, 5, 4, 3, 2, 1, 0], [7, 6, 5, 4, 3, 2], 0),
+                                         ([-9, 2, 100, 3, -1], [0, 1, 2, 3, 4, 5, 6, 7], list(range(8)), 0),
+                                         ([0, 3, 4, 5, 8], [5, 8, 0, 2 ** 31 - 1, -1, 1, 2, -2 ** 31], [5, 0, 1, 2], 2),
+                                         ([3, 3, 3, 3, 3], [0] * 8, [], 0)):
+        c.device_start, c.device_members, c.shared = dev(start), dev(members), dev([64] * 4)
+        out = c.call(ctx, q, empty(c, 4, "f16", 7.0), 0.1)
+        check(out[inside], *(x[inside] for x in want), "f16", 64)
+        assert (out[[b for b in range(8) if b not in inside]] == 7.0).all()
+        assert pq.pq_paged_device_error(ctx.handle) == told
+
+
+def test_blocks_that_are_not_there_and_values_that_are_no_numbers():
+    """A block outside the cache counts as no tokens, for all that would read it; NaN scales reach those that read them, no others."""
+    rng = np.random.default_rng(22)
+    c = Groups(rng, [(128, [128, 200, 300]), (128, [150, 160])], 2, 128, 16, order=False)
+    c.table[:3, 2] = -1
+    c.table[1, 9] = c.n_blocks
+    c.table[4, 8] = 2 ** 31 - 1
+    c.block_table.copy_(dev(c.table))
+    ctx = c.context("f16", 4, 2)
+    q, values = queries(rng, 5, 4, 128, "f16")
+    check(c.call(ctx, q, empty(c, 4, "f16"), 0.1), *c.expected(values, 0.1), "f16", 128)
+    assert pq.pq_paged_device_error(ctx.handle) == 2
+    before = c.call(ctx, q, empty(c, 4, "f16"), 0.1).clone()
+    c.scale["v"][int(c.table[1, 8])] = float("nan")           # of the second member alone
+    c.scale["k"][int(c.table[3, 3]), 1] = float("nan")        # of the second group, one head
+    out = c.call(ctx, q, empty(c, 4, "f16"), 0.1)
+    assert out[1].isnan().all() and out[3:, 2:].isnan().all()
+    assert torch.equal(out[[0, 2]], before[[0, 2]]) and torch.equal(out[3:, :2], before[3:, :2])
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.2, 4.0])
+def test_scores_of_all_sizes(scale):
+    rng = np.random.default_rng(23)
+    for dtype in ("f16", "bf16", "f32"):
+        c = Groups(rng, [(512, [700, 513, 2000]), (256, [300, 256])], 1, 128, 16)
+        for kind in "kv":
+            factor = np.exp2(rng.integers(-12, 6, c.model[kind].scale.shape)).astype(np.float32)
+            c.model[kind].scale *= factor
+            c.scale[kind].copy_(torch.from_numpy(c.model[kind].scale))
+        ctx = c.context(dtype, 2, 1)
+        q, values = queries(rng, c.seqs, 2, 128, dtype)
+        check(c.call(ctx, q, empty(c, 2, dtype), scale), *c.expected(values, scale), dtype, 128, dtype)
+
+
+def test_many_requests_of_one_token():
+    rng = np.random.default_rng(24)
+    c = Groups(rng, [(16, [16 + (i % 3) for i in range(3000)]), (0, [1] * 1000), (16, [17] * 96)], 1, 64, 16)
+    ctx = c.context("f16", 2, 1)
+    q, values = queries(rng, c.seqs, 2, 64, "f16")
+    check(c.call(ctx, q, empty(c, 2, "f16"), 0.1), *c.expected(values, 0.1), "f16", 64)
+    c = Groups(rng, [(16 * (i % 2), [16 + i % 5]) for i in range(4096)], 1, 64, 16)
+    ctx = c.context("f16", 1, 1)
+    q, values = queries(rng, c.seqs, 1, 64, "f16")
+    check(c.call(ctx, q, empty(c, 1, "f16"), 0.1), *c.expected(values, 0.1), "f16", 64)
+
+
+def test_the_same_as_decode_within_what_a_rounding_allows():
+    rng = np.random.default_rng(25)
+    for dtype, step in (("f16", 2.0 ** -10), ("f32", 2.0 ** -19)):
+        c = Groups(rng, [(4096, [4096 + 37 * i for i in range(20)]), (512, [600] * 5)], 4, 128, 32)
+        ctx = c.context(dtype, 16, 4)
+        q, _ = queries(rng, c.seqs, 16, 128, dtype)
+        out, plain = c.call(ctx, q, empty(c, 16, dtype), 0.09), empty(c, 16, dtype)
+        pq.pq_paged_decode(ctx.handle, c.seqs, q, q.shape[1], *c.cache(), 0.09, plain)
+        values = c.model["v"].scale[np.unique(c.table[c.table >= 0])].max() * 127
+        # each is off by its weights' rounding, of the sum of the values' sizes, and half a step of its own type
+        assert (out.double() - plain.double()).abs().max().item() <= 2 * step * values
+
+
+def test_a_graph_follows_lengths_groups_and_tables():
+    rng = np.random.default_rng(26)
+    c = Groups(rng, [(640, [700, 650, 900]), (160, [160, 200]), (0, [50]), (320, [330, 340])], 2, 128, 16)
+    ctx = c.context("f16", 8, 2)
+    workspace, out = work(ctx, c.seqs, 4), empty(c, 8, "f16")
+    q, values = queries(rng, c.seqs, 8, 128, "f16")
+    c.call(ctx, q, out, 0.1, workspace)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        c.call(ctx, q, out, 0.1, workspace)
+    for step in range(5):
+        t, values = queries(rng, c.seqs, 8, 128, "f16")
+        q.copy_(t)
+        keep = np.minimum(c.lengths, rng.integers(0, 1000, c.seqs)) if step else c.lengths
+        c.lengths = keep
+        c.seq_len.copy_(dev(keep))
+        c.shared.copy_(dev([s // (step + 1) for s, _ in c.groups]))
+        if step == 3:
+            c.device_start.copy_(dev([0, 1, 1, 2, 3]))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        inside = c.members[:3] if step >= 3 else c.members
+        check(out[inside.tolist()], *(x[inside] for x in c.expected(values, 0.1)), "f16", 128, f"replay {step}")
+        if step >= 3:
+            assert (out[c.members[3:].tolist()] == 7.0).all()
+        again = c.call(ctx, q, empty(c, 8, "f16", 7.0), 0.1)   # eager, a workspace of its own
+        torch.cuda.synchronize()
+        assert torch.equal(again, out)
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    rng = np.random.default_rng(27)
+    c = Groups(rng, [(6000 // 16 * 16, [6100 + i for i in range(12)])], 2, 128, 16)
+    ctx = c.context("f16", 8, 2)
+    calls = []
+    for _ in range(2):
+        q, values = queries(rng, c.seqs, 8, 128, "f16")
+        calls.append((q, c.expected(values, 0.1), empty(c, 8, "f16"), work(ctx, c.seqs, 1), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for q, _, out, workspace, stream in calls:
+            with torch.cuda.stream(stream):
+                c.call(ctx, q, out, 0.1, workspace)
+    torch.cuda.synchronize()
+    for _, want, out, _, _ in calls:
+        check(out, *want, "f16", 128)
+
+
+def refused(status, call, *args):
+    with pytest.raises(pq.PQAttnError) as e:
+        call(*args)
+    assert e.value.status == status
+
+
+def test_refusals_launch_nothing():
+    NULL, SHAPE, CAPACITY = -1, -2, -4
+    rng = np.random.default_rng(28)
+    c = Groups(rng, [(32, [40, 50]), (0, [20])], 2, 64, 16)
+    ctx = c.context("f16", 4, 2)
+    h, out, workspace = ctx.handle, empty(c, 4, "f16", 7.0), work(ctx, 3, 2)
+    q, _ = queries(rng, 3, 4, 64, "f16")
+    off = torch.zeros(100, dtype=torch.uint8, device="cuda")[2:]
+    args = [q, q.shape[1], *c.cache(), c.device_members, c.device_start, c.shared, 0.1, workspace, workspace.numel(), out]
+    for i in (0, 2, 3, 4, 5, 6, 7, 9, 10, 12, 14):
+        refused(NULL, pq.pq_paged_shared_decode, h, 3, 2, *args[:i], None, *args[i + 1:])
+    refused(NULL, pq.pq_paged_shared_decode, None, 3, 2, *args)
+    for n, groups, status in ((0, 1, SHAPE), (-1, 1, SHAPE), (4, 2, CAPACITY), (3, 0, SHAPE), (3, -1, SHAPE), (3, 4, CAPACITY)):
+        refused(status, pq.pq_paged_shared_decode, h, n, groups, *args)
+        refused(status, pq.pq_paged_shared_workspace_bytes, h, n, groups)
+    for i, bad, status in ((0, off, SHAPE), (1, 255, SHAPE), (1, 260, SHAPE), (1, 2 ** 31, SHAPE), (2, off, SHAPE), (3, off, SHAPE),
+                           (11, float("nan"), SHAPE), (11, 3e38, SHAPE), (12, off, SHAPE), (13, workspace.numel() - 1, CAPACITY),
+                           (13, 0, CAPACITY), (14, off, SHAPE)):
+        refused(status, pq.pq_paged_shared_decode, h, 3, 2, *args[:i], bad, *args[i + 1:])
+    torch.cuda.synchronize()
+    assert (out == 7.0).all() and (workspace == 255).all() and pq.pq_paged_device_error(h) == 0
