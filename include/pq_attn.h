@@ -441,7 +441,8 @@ int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const 
 
 /* pq_paged_decode for groups of requests that begin with the same blocks: those are read once for a group.
  *
- *   n_groups     1 .. n_seqs (PQ_ERR_SHAPE, PQ_ERR_CAPACITY otherwise)
+ *   n_groups     1 .. n_seqs (PQ_ERR_SHAPE, PQ_ERR_CAPACITY otherwise); n_seqs * ceil(Hq / Hkv / 16) * max_blocks *
+ *                block_tokens < 2^35 (PQ_ERR_CAPACITY)
  *   members      device [n_seqs] int32  requests, group after group, each at most once; NULL: 0, 1, .., n_seqs - 1
  *   group_start  device [n_groups + 1] int32  group g is members[group_start[g]] .. members[group_start[g + 1] - 1] (not
  *                ascending: a group that would begin before the one in front of it begins where that does)

@@ -60,7 +60,11 @@ int check_tokens(const pq_paged_ctx *ctx, int32_t n_tokens)
 int check_groups(const pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups)
 {
     const int rc = check_seqs(ctx, n_seqs);
-    return rc != PQ_OK ? rc : n_groups < 1 ? PQ_ERR_SHAPE : n_groups > n_seqs ? PQ_ERR_CAPACITY : PQ_OK;
+    if (rc != PQ_OK || n_groups < 1)
+        return rc != PQ_OK ? rc : PQ_ERR_SHAPE;
+    // steps of 32 tokens for up to 16 query heads of a KV head are numbered in 30 bits
+    const int64_t tiles = (ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads + 15) / 16, width = (int64_t)ctx->cfg.max_blocks << ctx->log_block;
+    return n_groups > n_seqs || n_seqs * tiles * width >= (int64_t)1 << 35 ? PQ_ERR_CAPACITY : PQ_OK;
 }
 
 int check_attention(const pq_paged_ctx *ctx, const void *q, int64_t q_stride, const uint8_t *k, const uint8_t *v, float scale, const void *out)
@@ -504,7 +508,7 @@ int pq_paged_shared_decode(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups, 
     if (!aligned(workspace))
         return PQ_ERR_SHAPE;
     pq_paged_shared_args a;
-    if (workspace_bytes < pq_paged_shared_layout(ctx, n_seqs, n_groups, workspace, &a.w))
+    if (workspace_bytes < pq_paged_shared_layout(ctx, n_seqs, n_groups, workspace, &a))
         return PQ_ERR_CAPACITY;
     device_guard guard(ctx->cfg.device);
     if (!guard.ok)
@@ -521,7 +525,6 @@ int pq_paged_shared_decode(pq_paged_ctx *ctx, int32_t n_seqs, int32_t n_groups, 
     a.n_groups = n_groups;
     a.Hq = ctx->cfg.n_q_heads;
     a.G = ctx->cfg.n_q_heads / ctx->cfg.n_kv_heads;
-    a.budget = pq_paged_shared_budget(ctx);
     return pq_launch_paged_shared(ctx, a, (hipStream_t)hip_stream) == hipSuccess ? PQ_OK : PQ_ERR_HIP;
 }
 

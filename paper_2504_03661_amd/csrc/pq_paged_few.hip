@@ -10,12 +10,12 @@
 // the conversion of bytes, which every tile of 32 rows does for itself: 1000 tokens over 8K keys 195 us, 663 TFLOP/s.
 #include <hip/hip_runtime.h>
 
-#include "pq_paged_step.h"
+#include "pq_paged_rows32.h"
 #include "pq_paged_work.h"
 
 namespace {
 
-constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = PQ_PAGED_FEW_ROWS, STEP = STEP_KEYS;
+constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = PQ_PAGED_FEW_ROWS, STEP = STEP_32;
 
 template <typename T, int D>
 __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_kernel(pq_paged_attn_args a, pq_paged_prefill_plan w)
@@ -84,6 +84,7 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_few_
             }
     }
 
+    // (rows_32 is the same loop; through it the compiler finds another order, with which chunks of prompts take 29.0 us instead of 28.6)
     f32x16 o[DT];
 #pragma unroll
     for (int i = 0; i < DT; ++i)

@@ -1,36 +1,108 @@
 // pq_paged_shared_decode: one query token per sequence, where groups of sequences begin with the same blocks.
 //
 // A group's query rows (a member's query heads of a KV head side by side, member after member) attend over the shared tokens in
-// tiles of 32 rows, so that a block's bytes are read and converted for 32 rows at once; what a member has behind them it attends
-// over by itself.  Both are the same work: a tile of rows over a piece of the keys of one block table, 32x32x16 products, the piece
-// shared out over four wavefronts.  A first launch (one workgroup) cuts the call into such jobs of about equal length, a second does
-// them, a third puts every row's pieces together:  with base_i, l_i, o_i of piece i,
+// tiles of 32 rows, so that a block's bytes are read and converted for 32 rows at once: a workgroup has a tile and a piece of
+// the keys, which its four wavefronts share out.  What the members have behind them they attend over by themselves, up to 16 rows
+// a tile.  All sequences' own tokens are one line, 32 at a step, and a wavefront has a range of it: as many steps as any other,
+// whatever the lengths are, and it goes from one sequence to the next where they end.  Both in one launch, cut so that
+// the chip is filled once; a second one puts every row's pieces together:  with base_i, l_i, o_i of piece i,
 //     m = max base_i,   out = sum 2^(base_i - m) o_i / sum 2^(base_i - m) l_i.
 #include <hip/hip_runtime.h>
 
+#include "pq_paged_rows16.h"
+#include "pq_paged_rows32.h"
 #include "pq_paged_scan.h"
 #include "pq_paged_shared.h"
-#include "pq_paged_step.h"
 
 namespace {
 
-constexpr int WAVES = 4, THREADS = 64 * WAVES, ROWS = PQ_PAGED_SHARED_ROWS, STEP = STEP_KEYS;
-constexpr int KEY_ALIGN = WAVES * STEP, LEAST_KEYS = 256;
+constexpr int WAVES = JOIN_WAVES, THREADS = 64 * WAVES, STEP = STEP_32;
+constexpr int GROUP_ROWS = JOIN_ROWS, OWN_ROWS = 16;  // of a tile
+constexpr int SMALL_SEQS = 64;                        // a call of up to so many sequences needs no launch that plans it
+static_assert(STEP_16 == STEP);
 
-struct shared_sums {
-    int start[PQ_PAGED_MAX_SEQS + 1];   // first position of each group
-    int shared[PQ_PAGED_MAX_SEQS];      // tokens that its members share
-    int length[PQ_PAGED_MAX_SEQS];      // of the sequence at a position; -1: none
-    int group_jobs[PQ_PAGED_MAX_SEQS + 1], own_jobs[PQ_PAGED_MAX_SEQS + 1];
-    int group_rows[PQ_PAGED_MAX_SEQS], own_rows[PQ_PAGED_MAX_SEQS];
-};
+__device__ inline int group_tiles(int rows) { return (rows + GROUP_ROWS - 1) / GROUP_ROWS; }
+__host__ __device__ inline int own_tiles(int G) { return (G + OWN_ROWS - 1) / OWN_ROWS; }
+__device__ inline int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
 
-__device__ inline int tiles_of(int rows) { return (rows + ROWS - 1) / ROWS; }
+// ---------------------------------------------------------------------------------------------------------- cutting
 
-// The pieces that n tokens are cut into, none longer than `most`, and their length.  (KEY_ALIGN divides `most`, so the rounded
+constexpr int GROUP_ALIGN = WAVES * STEP;
+constexpr int LEAST_STEPS = 2;  // of a range
+
+// A sequence's place on the line, from the steps that it has: whole shortest ranges, so that in a call that has no more than those
+// none goes from one sequence to the next.
+__device__ inline int place_of(int steps) { return (steps + LEAST_STEPS - 1) / LEAST_STEPS * LEAST_STEPS; }
+
+// Keys of a group's piece at most, from the keys over tiles of groups and sequences alike: a wavefront's share of all.  (The sum
+// is one in fp32: the pieces are taken a little larger, so that they are not more.)
+__device__ inline int group_piece(float keys, int workgroups)
+{
+    const int n = (int)fminf(keys * 1.0001f / (float)workgroups, (float)PQ_MAX_TOKENS) + 1;
+    return (n + GROUP_ALIGN - 1) / GROUP_ALIGN * GROUP_ALIGN;
+}
+
+// How many pieces n keys are cut into, none longer than `most`, and their length.  (GROUP_ALIGN divides `most`, so the rounded
 // length is no more than that, and n is behind (pieces - 1) * most: none is empty.)
 __device__ inline int pieces_of(int n, int most) { return (n + most - 1) / most; }
-__device__ inline int piece_length(int n, int pieces) { return ((n + pieces - 1) / pieces + KEY_ALIGN - 1) / KEY_ALIGN * KEY_ALIGN; }
+__device__ inline int piece_length(int n, int pieces) { return ((n + pieces - 1) / pieces + GROUP_ALIGN - 1) / GROUP_ALIGN * GROUP_ALIGN; }
+
+__device__ inline int range_begin(const pq_paged_shared_ranges &r, int w)
+{
+    return w <= r.n_longer ? w * r.longer : r.n_longer * r.longer + (w - r.n_longer) * r.shorter;
+}
+
+__device__ inline int range_of(const pq_paged_shared_ranges &r, int step)
+{
+    const int behind = step - r.n_longer * r.longer;
+    return behind < 0 ? step / r.longer : r.n_longer + behind / r.shorter;
+}
+
+// The line's `steps` over the workgroups that the groups' jobs leave: those that run beside them get longer ranges, those that take
+// their place when they are done shorter ones, by what the jobs' wavefronts have to do, so that all end together.
+__device__ inline pq_paged_shared_ranges cut_line(int steps, float group_keys, int group_jobs, int workgroups)
+{
+    pq_paged_shared_ranges r;
+    const int beside = workgroups - group_jobs;
+    const float all = (float)(WAVES * workgroups), of_job = group_jobs > 0 ? group_keys / (float)(WAVES * STEP * group_jobs) : 0.0f;
+    const float longer = ((float)steps + (float)(WAVES * group_jobs) * of_job) / all, shorter = longer - of_job;
+    if (group_jobs > 0 && beside > 0 && shorter >= (float)LEAST_STEPS) {
+        r.n_longer = WAVES * beside;
+        r.longer = (int)(longer * 1.0001f) + 1;
+        r.shorter = (int)(shorter * 1.0001f) + 1;
+    } else {
+        const int waves = WAVES * (beside > 0 ? beside : workgroups), each = (steps + waves - 1) / waves;
+        r.longer = r.shorter = each > LEAST_STEPS ? each : LEAST_STEPS;
+        r.n_longer = 0;
+    }
+    const int in_longer = r.n_longer * r.longer;
+    r.count = steps <= in_longer ? (steps + r.longer - 1) / r.longer : r.n_longer + (steps - in_longer + r.shorter - 1) / r.shorter;
+    return r;
+}
+
+// Job `at` of a group: `rows` query rows from position `first` on, over its shared tokens.  Tiles of one piece side by side: they read the
+// same bytes.
+__device__ inline void group_job(pq_paged_shared_job &job, int first, int rows, int shared, int pieces, int partial, int at)
+{
+    const int tiles = group_tiles(rows), piece = at / tiles, tile = at - piece * tiles, keys = piece_length(shared, pieces);
+    job.position = job.table = first;
+    job.row0 = tile * GROUP_ROWS;
+    job.rows = rows - job.row0 < GROUP_ROWS ? rows - job.row0 : GROUP_ROWS;
+    job.k0 = piece * keys;
+    job.k1 = job.k0 + keys < shared ? job.k0 + keys : shared;
+    job.partial = partial + job.row0 * pieces + piece * job.rows;
+}
+
+// -------------------------------------------------------------------------------------- the plan, by one workgroup
+
+struct shared_sums {
+    int start[PQ_PAGED_MAX_SEQS + 1];        // first position of each group
+    int shared[PQ_PAGED_MAX_SEQS];           // tokens that its members share
+    int length[PQ_PAGED_MAX_SEQS];           // of the sequence at a position; -1: none
+    int group_jobs[PQ_PAGED_MAX_SEQS + 1];
+    int group_rows[PQ_PAGED_MAX_SEQS];
+    int begin[PQ_PAGED_MAX_SEQS + 1];        // of the sequences that have tokens of their own, on their line
+};
 
 // inclusive maximum over the workgroup's threads
 __device__ inline int scan_max(int x, scan_room &room)
@@ -67,8 +139,13 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
 {
     __shared__ shared_sums s;
     __shared__ scan_room room;
-    __shared__ float float_room[SCAN_WAVES];
-    const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G;
+    __shared__ float float_room[2][SCAN_WAVES];
+    const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G, tiles = own_tiles(G);
+    bool range = false;
+    for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS) {
+        const int b = a.members == nullptr ? i : a.members[i];
+        s.length[i] = (unsigned)b < (unsigned)n_seqs ? paged_length(a.c, b) : -2;
+    }
     // where groups begin: as they are given, but never before the one in front
     int highest = 0;
     for (int g0 = 0; g0 <= n_groups; g0 += SCAN_THREADS) {
@@ -82,18 +159,15 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
         highest = s.start[g0 + SCAN_THREADS - 1 < n_groups ? g0 + SCAN_THREADS - 1 : n_groups];
         __syncthreads();
     }
-    bool range = false;
     for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS) {
-        const int b = a.members == nullptr ? i : a.members[i];
-        const bool there = (unsigned)b < (unsigned)n_seqs;
         const bool in_group = i >= s.start[0] && i < s.start[n_groups];
-        s.length[i] = in_group && there ? paged_length(a.c, b) : -1;
-        range |= in_group && !there;
+        range |= in_group && s.length[i] == -2;
+        s.length[i] = in_group && s.length[i] >= 0 ? s.length[i] : -1;
     }
     if (range)
         paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
     __syncthreads();
-    float work = 0.0f;
+    float of_groups = 0.0f, of_own = 0.0f;
     for (int g = threadIdx.x; g < n_groups; g += SCAN_THREADS) {
         const int first = s.start[g], n = s.start[g + 1] - first;
         int shared = 0;
@@ -103,17 +177,19 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
             shared = shared > 0 ? shared >> a.c.log_block << a.c.log_block : 0;
         }
         s.shared[g] = shared;
-        work += (float)tiles_of(n * G) * (float)shared;
+        of_groups += (float)group_tiles(n * G) * (float)shared;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS)
         if (s.length[i] > 0) {
             const int own = s.length[i] - s.shared[owner(s.start, n_groups, i)];
-            work += own > 0 ? (float)tiles_of(G) * (float)own : 0.0f;
+            of_own += own > 0 ? (float)tiles * (float)own : 0.0f;
         }
-    const int most = piece_tokens(sum_all(work, float_room), a.budget, KEY_ALIGN, LEAST_KEYS);
+    of_groups = sum_all(of_groups, float_room[0]);
+    of_own = sum_all(of_own, float_room[1]);
+    const int most = group_piece(of_groups + of_own, a.workgroups);
 
-    // jobs and rows of partials: of the groups first, then of the members by themselves
+    // jobs and rows of partials of the groups
     int jobs = 0, rows = 0;
     for (int g0 = 0; g0 < n_groups; g0 += SCAN_THREADS) {
         const int g = g0 + threadIdx.x;
@@ -122,7 +198,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
             n = (s.start[g + 1] - s.start[g]) * G;
             pieces = pieces_of(s.shared[g], most);
         }
-        int upto = tiles_of(n) * pieces, upto_rows = n * pieces, all, all_rows;
+        int upto = group_tiles(n) * pieces, upto_rows = n * pieces, all, all_rows;
         const int mine = upto, mine_rows = upto_rows;
         scan_two(upto, upto_rows, room, all, all_rows);
         if (g < n_groups) {
@@ -132,250 +208,286 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
         jobs += all;
         rows += all_rows;
     }
-    const int of_groups = jobs;
+    if (threadIdx.x == 0)
+        s.group_jobs[n_groups] = jobs;
+    __syncthreads();
+    // the line of the sequences' own tokens
+    int line = 0, n_own = 0;
     for (int i0 = 0; i0 < n_seqs; i0 += SCAN_THREADS) {
         const int i = i0 + threadIdx.x;
-        int pieces = 0, g = 0;
+        int g = 0, own = 0;
         if (i < n_seqs && s.length[i] >= 0) {
             g = owner(s.start, n_groups, i);
-            const int own = s.length[i] - s.shared[g];
-            pieces = own > 0 ? pieces_of(own, most) : 0;
+            own = s.length[i] - s.shared[g];
         }
-        int upto = tiles_of(G) * pieces, upto_rows = G * pieces, all, all_rows;
-        const int mine = upto, mine_rows = upto_rows;
-        scan_two(upto, upto_rows, room, all, all_rows);
+        const int steps = own > 0 ? steps_of(own) : 0, place = tiles * place_of(steps);
+        int upto = place, number = steps > 0, all, all_own;
+        scan_two(upto, number, room, all, all_own);
+        const int begin = line + upto - place, at = n_own + number - 1;
         if (i < n_seqs) {
-            s.own_jobs[i] = upto - mine + jobs - of_groups;
-            s.own_rows[i] = rows + upto_rows - mine_rows;
             pq_paged_shared_member m;
             m.b = s.length[i] < 0 ? -1 : a.members == nullptr ? i : a.members[i];
-            m.own_row = s.own_rows[i];
-            m.own_pieces = pieces;
             m.row = (i - s.start[g]) * G;
             m.rows = (s.start[g + 1] - s.start[g]) * G;
             m.group_row = s.group_rows[g];
             m.group_pieces = m.b < 0 ? 0 : pieces_of(s.shared[g], most);
-            m.unused = 0;
+            m.own = steps > 0 ? at : -1;
+            m.begin = begin;
+            m.steps = steps;
             a.w.members[i] = m;
+            if (steps > 0) {
+                pq_paged_shared_own o;
+                o.b = m.b;
+                o.k0 = s.shared[g];
+                o.k1 = s.length[i];
+                o.begin = begin;
+                a.w.own[at] = o;
+                s.begin[at] = begin;
+            }
         }
-        jobs += all;
-        rows += all_rows;
+        line += all;
+        n_own += all_own;
     }
+    const pq_paged_shared_ranges ranges = cut_line(line, of_groups, jobs, a.workgroups);
     if (threadIdx.x == 0) {
-        s.group_jobs[n_groups] = of_groups;
-        s.own_jobs[n_seqs] = jobs - of_groups;
-        a.w.head[0] = jobs;
+        pq_paged_shared_head head;
+        head.group_jobs = jobs;
+        head.group_rows = rows;
+        head.n_own = n_own;
+        head.ranges = ranges;
+        *a.w.head = head;
     }
     __syncthreads();
+    for (int w = threadIdx.x; w < ranges.count; w += SCAN_THREADS)
+        a.w.first[w] = owner(s.begin, n_own, range_begin(ranges, w));
     for (int e = threadIdx.x; e < jobs; e += SCAN_THREADS) {
+        const int g = owner(s.group_jobs, n_groups, e);
         pq_paged_shared_job job;
-        if (e < of_groups) {
-            const int g = owner(s.group_jobs, n_groups, e), at = e - s.group_jobs[g];
-            const int n = (s.start[g + 1] - s.start[g]) * G, tiles = tiles_of(n), pieces = pieces_of(s.shared[g], most);
-            // tiles of one piece side by side: they read the same bytes
-            const int piece = at / tiles, tile = at - piece * tiles, keys = piece_length(s.shared[g], pieces);
-            job.position = s.start[g];
-            job.table = s.start[g];
-            job.row0 = tile * ROWS;
-            job.rows = n - job.row0 < ROWS ? n - job.row0 : ROWS;
-            job.k0 = piece * keys;
-            job.k1 = job.k0 + keys < s.shared[g] ? job.k0 + keys : s.shared[g];
-            job.partial = s.group_rows[g] + job.row0 * pieces + piece * job.rows;
-        } else {
-            const int i = owner(s.own_jobs, n_seqs, e - of_groups), at = e - of_groups - s.own_jobs[i];
-            const int shared = s.shared[owner(s.start, n_groups, i)], own = s.length[i] - shared, tiles = tiles_of(G);
-            const int pieces = pieces_of(own, most), piece = at / tiles, tile = at - piece * tiles, keys = piece_length(own, pieces);
-            job.position = job.table = i;
-            job.row0 = tile * ROWS;
-            job.rows = G - job.row0 < ROWS ? G - job.row0 : ROWS;
-            job.k0 = shared + piece * keys;
-            job.k1 = job.k0 + keys < s.length[i] ? job.k0 + keys : s.length[i];
-            job.partial = s.own_rows[i] + job.row0 * pieces + piece * job.rows;
-        }
+        group_job(job, s.start[g], (s.start[g + 1] - s.start[g]) * G, s.shared[g], pieces_of(s.shared[g], most), s.group_rows[g],
+                  e - s.group_jobs[g]);
         job.table = a.members == nullptr ? job.table : a.members[job.table];
         a.w.jobs[e] = job;
     }
 }
 
-template <typename T, int D>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shared_kernel(pq_paged_shared_args a)
-{
-    constexpr bool SPLIT = sizeof(T) == 4;  // two fp16 parts of queries and weights
-    constexpr int PARTS = SPLIT ? 2 : 1, DT = D / 32;
-    __shared__ float part[WAVES][ROWS][D + 4];
-    __shared__ float wave_base[WAVES][ROWS], wave_l[WAVES][ROWS], row_base[ROWS], row_l[ROWS];
+// ------------------------------------------------------------------------------- the plan of a small call, by a wavefront
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
-    const int h = blockIdx.x % a.c.Hkv, e = blockIdx.x / a.c.Hkv;
-    if (e >= a.w.head[0])
-        return;
-    const pq_paged_shared_job job = a.w.jobs[e];
-    const int share = ((job.k1 - job.k0 + WAVES - 1) / WAVES + STEP - 1) / STEP * STEP;
-    const int t0 = job.k0 + wave * share, t1 = t0 + share < job.k1 ? t0 + share : job.k1;
-    const int32_t *table = a.c.table + (int64_t)job.table * a.c.max_blocks;
-    const int last_block = (job.k1 + (1 << a.c.log_block) - 1) >> a.c.log_block;
-    step_bytes<D> now, next;
+// Lane g has group g, lane i the sequence at position i.
+struct small_plan {
+    int lo, rows, shared, group_pieces, group_job, group_row;  // first position, query rows, tokens, pieces, first job, first partial
+    int b, length, group, steps, begin;                        // steps of its own, of one tile, and where they begin on the line
+    pq_paged_shared_head head;
+};
+
+__device__ inline int running_max(int x, int lane)
+{
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(x, d, 64);
+        x = lane >= d && y > x ? y : x;
+    }
+    return x;
+}
+
+__device__ inline int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+__device__ inline small_plan plan_small(const pq_paged_shared_args &a, int lane)
+{
+    small_plan p;
+    const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G, tiles = own_tiles(G);
+    const bool is_group = lane < n_groups, is_seq = lane < n_seqs;
+    int lo = is_group ? a.group_start[lane] : 0, hi = is_group ? a.group_start[lane + 1] : 0;
+    int asked = is_group ? a.shared_len[lane] : 0;
+    p.b = !is_seq ? -1 : a.members == nullptr ? lane : a.members[lane];
+    const bool there = (unsigned)p.b < (unsigned)n_seqs;
+    const int length = there ? paged_length(a.c, p.b) : -1;
+    lo = running_max(between(lo, n_seqs), lane);
+    hi = between(hi, n_seqs);
+    hi = hi > lo ? hi : lo;
+    p.lo = lo;
+    p.rows = is_group ? (hi - lo) * G : 0;
+    const int begin = of_lane(lo, 0), end = of_lane(hi, n_groups - 1);
+    // the last group that begins at or before the position, by six halvings
+    int low = 0, high = n_groups;
+#pragma unroll
+    for (int k = 0; k < 6; ++k) {
+        const int mid = (low + high) >> 1, at = __shfl(lo, mid < 63 ? mid : 63, 64);
+        if (high - low > 1) {
+            low = at <= lane ? mid : low;
+            high = at <= lane ? high : mid;
+        }
+    }
+    p.group = low;
+    const bool in_group = is_seq && lane >= begin && lane < end;
+    p.length = in_group && there ? length : -1;
+    if (__ballot(in_group && !there) != 0 && lane == 0)
+        paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+    const int of_first = __shfl(p.length, lo < 63 ? lo : 63, 64);
+    asked = asked < of_first ? asked : of_first;
+    p.shared = p.rows > G && asked > 0 ? asked >> a.c.log_block << a.c.log_block : 0;
+    const int own = p.length - __shfl(p.shared, p.group, 64);
+    const float of_groups = wave_sum((float)group_tiles(p.rows) * (float)p.shared);
+    const float of_own = wave_sum(own > 0 ? (float)tiles * (float)own : 0.0f);
+    p.group_pieces = pieces_of(p.shared, group_piece(of_groups + of_own, a.workgroups));
+    p.steps = own > 0 ? steps_of(own) : 0;
+    const int jobs = group_tiles(p.rows) * p.group_pieces, rows = p.rows * p.group_pieces;
+    const int place = tiles * place_of(p.steps);
+    const int upto_jobs = lane_scan(jobs), upto_rows = lane_scan(rows), upto_steps = lane_scan(place);
+    p.group_job = upto_jobs - jobs;
+    p.group_row = upto_rows - rows;
+    p.begin = upto_steps - place;
+    p.head.group_jobs = of_lane(upto_jobs, 63);
+    p.head.group_rows = of_lane(upto_rows, 63);
+    p.head.n_own = n_seqs;  // (those without tokens of their own are numbered too)
+    p.head.ranges = cut_line(of_lane(upto_steps, 63), of_groups, p.head.group_jobs, a.workgroups);
+    return p;
+}
+
+// ---------------------------------------------------------------------------------------------------------- attention
+
+// Row of the partials that the first row of a tile of a sequence's own is, in a range: both numbers only grow along the line.
+__device__ inline int own_partial(const pq_paged_shared_head &head, int G, int tile_number, int range)
+{
+    return head.group_rows + (tile_number + range) * (G < OWN_ROWS ? G : OWN_ROWS);
+}
+
+// A tile of a sequence's query rows over keys of its own
+template <typename T, int D>
+__device__ inline void attend_own(const pq_paged_shared_args &a, int h, int lane, int b, int row0, int k0, int k1, int partial)
+{
+    const int32_t *table = a.c.table + (int64_t)b * a.c.max_blocks;
+    const int rows = a.G - row0 < OWN_ROWS ? a.G - row0 : OWN_ROWS;
+    const int last_block = (k1 + (1 << a.c.log_block) - 1) >> a.c.log_block, col = lane & 15, quad = lane >> 4;
     block_batch batch;
     batch.first = -65;
-    if (t0 < t1)
-        load_bytes<D>(a.c, table, batch, last_block, h, t0, lane, now);
+    query_16<T, D> row;
+    load_query((const T *)a.q + (int64_t)b * a.q_stride + (int64_t)(h * a.G + row0 + (col < rows ? col : 0)) * D, quad, row);
+    step_data<D> now;
+    load_step<D>(a.c, table, batch, last_block, h, k0, lane, now);
+    rows_16<T, D> r;
+    r.take(row, a.scale_log2e);
+    r.attend(a.c, table, batch, last_block, h, k0, k1, lane, now);
+    const float l = r.sum();
+    const int64_t to = (int64_t)h * a.w.most_rows + partial + col;
+    if (col < rows) {
+        if (quad == 0)
+            a.w.sums[to] = make_float2(r.base, l);
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+            *(f32x4 *)(a.w.partials + to * D + 16 * i + 4 * quad) = r.o[i];
+    }
+}
 
-    const int col = lane & 31, half = lane >> 5;
-    const int row = job.row0 + (col < job.rows ? col : 0), at = row / a.G, head = row - at * a.G;
-    const int b = a.members == nullptr ? job.position + at : a.members[job.position + at];
-    const bool there = (unsigned)b < (unsigned)a.n_seqs;
-    // (columns behind the last row repeat the first one, and nobody takes what they find)
-    int sees = col >= job.rows ? t1 : there ? paged_length(a.c, b) : 0;
-    sees = sees < t1 ? sees : t1;
-    const bool whole = __ballot(sees < t1) == 0;  // every row sees all of this wavefront's keys
-    half8v q[PARTS][D / 16];
-    float per_score;
-    {
-        // dims 32 x + 16 half + 0 .. 15 of the row, as K's loads bring them
-        float v[D / 2];
-        float high = 0.0f;
-        const T *src = (const T *)a.q + (int64_t)(there ? b : 0) * a.q_stride + (int64_t)(h * a.G + head) * D + 16 * half;
-#pragma unroll
-        for (int x = 0; x < D / 32; ++x) {
-            paged_load8(src + 32 * x, v + 16 * x);
-            paged_load8(src + 32 * x + 8, v + 16 * x + 8);
-        }
-#pragma unroll
-        for (int i = 0; i < D / 2; ++i)
-            high = fmaxf(high, fabsf(v[i]));
-        high = fmaxf(high, __shfl_xor(high, 32, 64));
-        const int exponent = query_exponent(high);
-        per_score = ldexpf(a.scale_log2e, -exponent);
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float f = ldexpf(v[8 * x + j], exponent);
-                q[0][x][j] = (_Float16)f;
-                if (SPLIT)
-                    q[PARTS - 1][x][j] = (_Float16)(f - (float)q[0][x][j]);
-            }
+// The part of range `range` that a sequence's own tokens, from step `begin` of the line on, have
+template <typename T, int D>
+__device__ inline void attend_range(const pq_paged_shared_args &a, const pq_paged_shared_head &head, int h, int lane, int range, int b, int k0,
+                                    int k1, int begin, int number)
+{
+    const int steps = steps_of(k1 - k0), place = place_of(steps), tiles = own_tiles(a.G);
+    const int from = range_begin(head.ranges, range) - begin, end = range_begin(head.ranges, range + 1) - begin;
+    for (int tile = from > 0 ? from / place : 0; tile < tiles && tile * place < end; ++tile) {
+        const int first = from > tile * place ? from - tile * place : 0, last = end - tile * place < steps ? end - tile * place : steps;
+        if (first < last)
+            attend_own<T, D>(a, h, lane, b, tile * OWN_ROWS, k0 + first * STEP, last < steps ? k0 + last * STEP : k1,
+                             own_partial(head, a.G, number * tiles + tile, range));
     }
+}
 
-    f32x16 o[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            o[i][j] = 0.0f;
-    float base = LOWEST, l = 0.0f;
-    for (int t = t0; t < t1; t += STEP) {
-        const bool more = t + STEP < t1;
-        if (more)
-            load_bytes<D>(a.c, table, batch, last_block, h, t + STEP, lane, next);
-        f32x16 dot;
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            dot[j] = 0.0f;
-#pragma unroll
-        for (int x = 0; x < D / 16; ++x) {
-            const half8v k = codes8(now.k[x >> 1][2 * (x & 1)], now.k[x >> 1][2 * (x & 1) + 1]);
-#pragma unroll
-            for (int i = 0; i < PARTS; ++i)
-                dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][x], dot, 0, 0, 0);
+template <typename T, int D, bool SMALL>
+__global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shared_kernel(pq_paged_shared_args a)
+{
+    __shared__ join_room<D> room;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int h = blockIdx.x % a.c.Hkv;
+    small_plan p;
+    if constexpr (SMALL) {
+        p = plan_small(a, lane);
+        if (blockIdx.x == 0 && wave == 0) {  // for the merge
+            const int lo = __shfl(p.lo, p.group, 64), rows = __shfl(p.rows, p.group, 64);
+            const int group_row = __shfl(p.group_row, p.group, 64), pieces = __shfl(p.group_pieces, p.group, 64);
+            if (lane < a.n_seqs)
+                a.w.members[lane] = pq_paged_shared_member{p.length < 0 ? -1 : p.b, (lane - lo) * a.G, rows, group_row, pieces,
+                                                           lane, p.begin, p.steps};
+            if (lane == 0)
+                *a.w.head = p.head;
         }
-        float s[16];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float by = per_score * now.k_scale[i];
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                s[8 * i + j] = fmaf(dot[8 * i + j], by, now.v_log[i]);
-        }
-        if (!whole || t + STEP > t1)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (t + 8 * (j >> 2) + 4 * half + (j & 3) >= sees)
-                    s[j] = -INFINITY;
-        float high = s[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j)
-            high = fmaxf(high, s[j]);
-        if (__ballot(high - base > MOST_BITS) != 0) {
-            high = fmaxf(high, __shfl_xor(high, 32, 64));
-            const float moved = fmaxf(base, weight_base(high)), down = __builtin_amdgcn_exp2f(base - moved);
-            base = moved;
-            l *= down;
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    o[i][j] *= down;
-        }
-        half8v weights[PARTS][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float sum = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float x = __builtin_amdgcn_exp2f(s[8 * i + j] - base);
-                sum += x;
-                weights[0][i][j] = (_Float16)x;
-                if (SPLIT)
-                    weights[PARTS - 1][i][j] = (_Float16)(x - (float)weights[0][i][j]);
+    } else {
+        p.head = *a.w.head;
+    }
+    // The groups' jobs first, then four ranges of the line at a time; the grid is what runs together
+    const int stride = gridDim.x / a.c.Hkv, jobs = p.head.group_jobs + (p.head.ranges.count + WAVES - 1) / WAVES;
+    for (int e = blockIdx.x / a.c.Hkv; e < jobs; e += stride) {
+        if (e >= p.head.group_jobs) {
+            const int range = (e - p.head.group_jobs) * WAVES + wave;
+            if (range >= p.head.ranges.count)
+                continue;
+            const int end = range_begin(p.head.ranges, range + 1);
+            if constexpr (SMALL) {
+                const int first = range_begin(p.head.ranges, range), upto = p.begin + own_tiles(a.G) * place_of(p.steps);
+                const int shared = __shfl(p.shared, p.group, 64);
+                // lanes whose sequences have a part of the range
+                for (uint64_t mine = __ballot(p.begin < end && upto > first && p.steps > 0); mine != 0; mine &= mine - 1) {
+                    const int i = __builtin_ctzll(mine);
+                    attend_range<T, D>(a, p.head, h, lane, range, of_lane(p.b, i), of_lane(shared, i), of_lane(p.length, i),
+                                       of_lane(p.begin, i), i);
+                }
+            } else {
+                for (int i = a.w.first[range]; i < p.head.n_own; ++i) {
+                    const pq_paged_shared_own o = a.w.own[i];
+                    if (o.begin >= end)
+                        break;
+                    attend_range<T, D>(a, p.head, h, lane, range, o.b, o.k0, o.k1, o.begin, i);
+                }
             }
-            l = fmaf(sum, now.v_inv[i], l);
+            continue;
         }
-#pragma unroll
-        for (int i = 0; i < DT; ++i)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const half8v v = codes8(now.v[x][0][i], now.v[x][1][i]);
-#pragma unroll
-                for (int j = 0; j < PARTS; ++j)
-                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[j][x], o[i], 0, 0, 0);
-            }
-        if (more)
-            now = next;
-    }
-
-    // the wavefronts' parts
-    l += __shfl_xor(l, 32, 64);
-    if (half == 0) {
-        wave_base[wave][col] = base;
-        wave_l[wave][col] = l;
-    }
-#pragma unroll
-    for (int i = 0; i < DT; ++i)
-#pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-            const int d = (D == 128 ? 64 * (j >> 3) + 16 * i : 32 * (j >> 3) + 16 * i) + 8 * ((j >> 2) & 1) + 4 * half;
-            *(f32x4 *)&part[wave][col][d] = f32x4{o[i][j], o[i][j + 1], o[i][j + 2], o[i][j + 3]};
+        const int col = lane & 31, half = lane >> 5;
+        pq_paged_shared_job job;
+        int row, at, b, length;  // this lane's query row, its member, and that one's sequence
+        if constexpr (SMALL) {
+            const int next = p.group_job + group_tiles(p.rows) * p.group_pieces;
+            const int g = __builtin_ctzll(__ballot(e >= p.group_job && e < next));
+            group_job(job, of_lane(p.lo, g), of_lane(p.rows, g), of_lane(p.shared, g), of_lane(p.group_pieces, g),
+                      of_lane(p.group_row, g), e - of_lane(p.group_job, g));
+            row = job.row0 + (col < job.rows ? col : 0);
+            at = row / a.G;
+            b = __shfl(p.b, job.position + at, 64);
+            length = __shfl(p.length, job.position + at, 64);
+            job.table = of_lane(p.b, job.table);
+        } else {
+            job = a.w.jobs[e];
+            row = job.row0 + (col < job.rows ? col : 0);
+            at = row / a.G;
+            b = a.members == nullptr ? job.position + at : a.members[job.position + at];
+            length = (unsigned)b < (unsigned)a.n_seqs ? paged_length(a.c, b) : -1;
         }
-    __syncthreads();
-    if (threadIdx.x < ROWS) {
-        const int r = threadIdx.x;
-        float top = wave_base[0][r], sum = 0.0f;
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i)
-            top = fmaxf(top, wave_base[i][r]);
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-            const float down = __builtin_amdgcn_exp2f(wave_base[i][r] - top);
-            sum = fmaf(wave_l[i][r], down, sum);
-            wave_base[i][r] = down;
+        query_32<T, D> query;
+        load_query((const T *)a.q + (int64_t)(length < 0 ? 0 : b) * a.q_stride + (int64_t)(h * a.G + row - at * a.G) * D, half, query);
+        const int share = ((job.k1 - job.k0 + WAVES - 1) / WAVES + STEP - 1) / STEP * STEP;
+        const int t0 = job.k0 + wave * share, t1 = t0 + share < job.k1 ? t0 + share : job.k1;
+        const int32_t *table = a.c.table + (int64_t)job.table * a.c.max_blocks;
+        const int last_block = (job.k1 + (1 << a.c.log_block) - 1) >> a.c.log_block;
+        step_bytes<D> now;
+        block_batch batch;
+        batch.first = -65;
+        if (t0 < t1)
+            load_bytes<D>(a.c, table, batch, last_block, h, t0, lane, now);
+        // (columns behind the last row repeat the first one, and nobody takes what they find)
+        int sees = col >= job.rows ? t1 : length;
+        sees = sees < t1 ? sees : t1;
+        const int least = __ballot(sees < t1) == 0 ? t1 : 0;
+        rows_32<T, D> r;
+        r.take(query, a.scale_log2e);
+        r.attend(a.c, table, batch, last_block, h, t0, t1, sees, least, lane, now);
+        room.join(r, wave, lane);
+        const int64_t to = (int64_t)h * a.w.most_rows + job.partial;
+        for (int i = threadIdx.x; i < job.rows * (D / 2); i += THREADS) {
+            const int r = i / (D / 2), d = i % (D / 2) * 2;
+            *(float2 *)(a.w.partials + (to + r) * D + d) = room.values(r, d);
+            if (d == 0)
+                a.w.sums[to + r] = make_float2(room.row_base[r], room.row_l[r]);
         }
-        row_base[r] = top;
-        row_l[r] = sum;
-    }
-    __syncthreads();
-    float *const to = a.w.partials + ((int64_t)h * a.w.most_rows + job.partial) * (D + 2);
-    for (int i = threadIdx.x; i < job.rows * (D / 2); i += THREADS) {
-        const int r = i / (D / 2), d = i % (D / 2) * 2;
-        float x = 0.0f, y = 0.0f;
-#pragma unroll
-        for (int k = 0; k < WAVES; ++k) {
-            x = fmaf(part[k][r][d], wave_base[k][r], x);
-            y = fmaf(part[k][r][d + 1], wave_base[k][r], y);
-        }
-        *(float2 *)(to + r * (D + 2) + 2 + d) = make_float2(x, y);
-        if (d == 0)
-            *(float2 *)(to + r * (D + 2)) = make_float2(row_base[r], row_l[r]);
+        __syncthreads();
     }
 }
 
@@ -390,20 +502,18 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
     if (i >= a.n_seqs)
         return;
     const pq_paged_shared_member m = a.w.members[i];
+    const pq_paged_shared_head whole = *a.w.head;
     if (m.b < 0)
         return;
     const int h = head / a.G, g = head - h * a.G;
-    const float *const partials = a.w.partials + (int64_t)h * a.w.most_rows * (D + 2);
     float top = LOWEST, sum = 0.0f, o[PER_LANE] = {};
-    // row r of `rows`, whose tile's pieces lie one after another
-    const auto add = [&](int first, int r, int rows, int pieces) {
-        const int tile = r / ROWS, in_tile = rows - tile * ROWS < ROWS ? rows - tile * ROWS : ROWS;
-        const float *from = partials + (int64_t)(first + tile * ROWS * pieces + (r - tile * ROWS)) * (D + 2);
-        const int64_t stride = (int64_t)in_tile * (D + 2);
-        for (int c0 = 0; c0 < pieces; c0 += 64, from += 64 * stride) {
+    // `pieces` partials of a row, the first one's row and how many rows they are apart
+    const auto add = [&](int first, int pieces, int stride) {
+        int64_t from = (int64_t)h * a.w.most_rows + first;
+        for (int c0 = 0; c0 < pieces; c0 += 64, from += 64 * (int64_t)stride) {
             // a lane has a piece's base and sum, and so its weight; one that is not there has the weight 0
             const int n = pieces - c0 < 64 ? pieces - c0 : 64;
-            const float2 ml = lane < n ? *(const float2 *)(from + lane * stride) : make_float2(-INFINITY, 0.0f);
+            const float2 ml = lane < n ? a.w.sums[from + lane * stride] : make_float2(-INFINITY, 0.0f);
             const float high = fmaxf(top, wave_max(ml.x)), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
             top = high;
             sum = fmaf(sum, old, wave_sum(ml.y * by));
@@ -417,7 +527,7 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
                 for (int c = 0; c < AT_ONCE; ++c)
 #pragma unroll
                     for (int d = 0; d < PER_LANE; ++d)
-                        v[c][d] = from[(c1 + c < n ? c1 + c : 0) * stride + 2 + PER_LANE * lane + d];
+                        v[c][d] = a.w.partials[(from + (c1 + c < n ? c1 + c : 0) * stride) * D + PER_LANE * lane + d];
 #pragma unroll
                 for (int c = 0; c < AT_ONCE; ++c) {
                     const float weight = lane_of(by, c1 + c);
@@ -428,8 +538,15 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
             }
         }
     };
-    add(m.group_row, m.row + g, m.rows, m.group_pieces);
-    add(m.own_row, g, a.G, m.own_pieces);
+    if (m.group_pieces > 0) {
+        const int r = m.row + g, row0 = r / GROUP_ROWS * GROUP_ROWS;
+        add(m.group_row + row0 * m.group_pieces + (r - row0), m.group_pieces, m.rows - row0 < GROUP_ROWS ? m.rows - row0 : GROUP_ROWS);
+    }
+    if (m.steps > 0) {
+        const int tile = g / OWN_ROWS, begin = m.begin + tile * place_of(m.steps);
+        const int first = range_of(whole.ranges, begin), pieces = range_of(whole.ranges, begin + m.steps - 1) - first + 1;
+        add(own_partial(whole, a.G, m.own * own_tiles(a.G) + tile, first) + g - tile * OWN_ROWS, pieces, a.G < OWN_ROWS ? a.G : OWN_ROWS);
+    }
     const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
     T *const out = (T *)a.out + ((int64_t)m.b * a.Hq + head) * D + PER_LANE * lane;
 #pragma unroll
@@ -437,49 +554,54 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
         out[d] = paged_elem<T>::down(o[d] * by);
 }
 
-int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
+constexpr int PER_CU = 2;  // workgroups that run together
 
 }  // namespace
 
-// Jobs: `budget` pieces and a rest for each tile.  Rows of partials: as many as the tiles of those pieces have.
-int64_t pq_paged_shared_layout(const pq_paged_ctx *ctx, int n_seqs, int n_groups, void *workspace, pq_paged_shared_work *w)
+// For each KV head: the groups' jobs are `workgroups` and a rest for each tile at most, the ranges of the line four for each workgroup, and
+// two that rounding adds; partials of the line have a row's place for each tile and each range.
+int64_t pq_paged_shared_layout(const pq_paged_ctx *ctx, int n_seqs, int n_groups, void *workspace, pq_paged_shared_args *a)
 {
     const pq_paged_config &cfg = ctx->cfg;
-    const int64_t G = cfg.n_q_heads / cfg.n_kv_heads, budget = pq_paged_shared_budget(ctx);
-    const int64_t tiles = n_seqs * G / ROWS + n_groups + n_seqs * ((G + ROWS - 1) / ROWS);
-    const int64_t jobs = budget + tiles, rows = ROWS * budget + 2 * n_seqs * G;
+    const int64_t G = cfg.n_q_heads / cfg.n_kv_heads;
+    const int filled = PER_CU * ctx->n_cu / cfg.n_kv_heads, workgroups = filled > 1 ? filled : 1;
+    const int64_t jobs = workgroups + n_seqs * G / GROUP_ROWS + n_groups, ranges = WAVES * workgroups + 2;
+    const int64_t rows = GROUP_ROWS * workgroups + n_seqs * G + (n_seqs * own_tiles(G) + ranges) * (G < OWN_ROWS ? G : OWN_ROWS);
     int64_t bytes = 0;
-    const auto room = [&](int64_t n) { const int64_t at = bytes; bytes += round_up(n); return at; };
-    const int64_t head_at = room(sizeof(int)), members_at = room(n_seqs * sizeof(pq_paged_shared_member));
-    const int64_t jobs_at = room(jobs * sizeof(pq_paged_shared_job));
-    const int64_t partials_at = room(cfg.n_kv_heads * rows * (cfg.head_dim + 2) * sizeof(float));
-    if (w != nullptr) {
+    const auto room = [&](int64_t n) { const int64_t at = bytes; bytes += (n + 255) / 256 * 256; return at; };
+    const int64_t head_at = room(sizeof(pq_paged_shared_head)), members_at = room(n_seqs * sizeof(pq_paged_shared_member));
+    const int64_t jobs_at = room(jobs * sizeof(pq_paged_shared_job)), own_at = room(n_seqs * sizeof(pq_paged_shared_own));
+    const int64_t first_at = room(ranges * sizeof(int)), sums_at = room(cfg.n_kv_heads * rows * sizeof(float2));
+    const int64_t partials_at = room(cfg.n_kv_heads * rows * cfg.head_dim * sizeof(float));
+    if (a != nullptr) {
         char *const at = (char *)workspace;
-        w->head = (int *)(at + head_at);
-        w->members = (pq_paged_shared_member *)(at + members_at);
-        w->jobs = (pq_paged_shared_job *)(at + jobs_at);
-        w->partials = (float *)(at + partials_at);
-        w->most_jobs = (int)jobs;
-        w->most_rows = rows;
+        a->w.head = (pq_paged_shared_head *)(at + head_at);
+        a->w.members = (pq_paged_shared_member *)(at + members_at);
+        a->w.jobs = (pq_paged_shared_job *)(at + jobs_at);
+        a->w.own = (pq_paged_shared_own *)(at + own_at);
+        a->w.first = (int *)(at + first_at);
+        a->w.sums = (float2 *)(at + sums_at);
+        a->w.partials = (float *)(at + partials_at);
+        a->w.most_rows = rows;
+        a->workgroups = workgroups;
     }
     return bytes;
 }
 
-// Pieces that a call's keys are cut into for each KV head: two workgroups a compute unit.
-int pq_paged_shared_budget(const pq_paged_ctx *ctx)
-{
-    const int n = 2 * ctx->n_cu / ctx->cfg.n_kv_heads;
-    return n > 1 ? n : 1;
-}
-
 hipError_t pq_launch_paged_shared(const pq_paged_ctx *ctx, const pq_paged_shared_args &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(pq_paged_shared_plan_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
-#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_shared_kernel<T, D>), dim3((unsigned)a.w.most_jobs * (unsigned)a.c.Hkv), dim3(THREADS), 0, s, a)
-    PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);
-#undef LAUNCH
-    const int64_t rows = (int64_t)a.n_seqs * a.Hq;
-#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_shared_merge_kernel<T, D>), dim3((unsigned)((rows + WAVES - 1) / WAVES)), dim3(THREADS), 0, s, a)
+    const bool small = a.n_seqs <= SMALL_SEQS;
+    if (!small)
+        hipLaunchKernelGGL(pq_paged_shared_plan_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
+    const dim3 grid((unsigned)a.workgroups * (unsigned)a.c.Hkv), rows((unsigned)(((int64_t)a.n_seqs * a.Hq + WAVES - 1) / WAVES));
+#define LAUNCH(T, D)                                                                                \
+    do {                                                                                            \
+        if (small)                                                                                  \
+            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, true>), grid, dim3(THREADS), 0, s, a);  \
+        else                                                                                        \
+            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, false>), grid, dim3(THREADS), 0, s, a); \
+        hipLaunchKernelGGL((pq_paged_shared_merge_kernel<T, D>), rows, dim3(THREADS), 0, s, a);      \
+    } while (0)
     PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);
 #undef LAUNCH
     return hipGetLastError();

@@ -277,6 +277,13 @@ def test_two_calls_at_once_with_a_workspace_each():
         check(out, *want, "f16", 128)
 
 
+def test_calls_whose_tokens_pass_what_is_numbered_are_refused():
+    for Hq, seqs, width, most in ((1, 4096, 1 << 20, 2047), (16, 4096, 1 << 20, 2047), (17, 2048, 1 << 20, 1023), (1024, 64, 1 << 20, 31)):
+        ctx = context("f16", Hq, 1, 64, 16, 100, width, seqs)
+        assert pq.pq_paged_shared_workspace_bytes(ctx.handle, most, 1) > 0
+        refused(-4, pq.pq_paged_shared_workspace_bytes, ctx.handle, most + 1, 1)
+
+
 def refused(status, call, *args):
     with pytest.raises(pq.PQAttnError) as e:
         call(*args)
