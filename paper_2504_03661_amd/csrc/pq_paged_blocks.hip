@@ -14,7 +14,8 @@
 namespace {
 
 constexpr int SEGMENTS = 256;  // of the block numbers, at most, each a workgroup's
-constexpr int ROW_THREADS = 256;
+constexpr int ROW_THREADS = 256, ROW_LOADS = 4;  // entries of a thread on their way together
+constexpr int ONE_ENTRIES = 4096;   // of all block tables together, up to which one workgroup does a call
 
 // what a call's launches hand over, in the context's scratch
 struct blocks_scratch {
@@ -30,10 +31,36 @@ __device__ inline int length_of(const int32_t *seq_len, int b, int most) { retur
 
 // ---------------------------------------------------------------------------------------------------------- fork
 
-// Who becomes whose fork, and the block that it needs for itself: one workgroup, a chunk of 1024 rows at a time.
-__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fork_args a)
+// Row b's shared blocks into its table, and counted, by threads first, first + step, ..  A row that gets blocks was empty: nobody
+// reads it.  Whether all numbers were in range.
+__device__ inline bool share_row(const pq_paged_fork_args &a, int b, int parent, int n, int first, int step)
 {
-    __shared__ int length[PQ_PAGED_MAX_SEQS];
+    const int32_t *from = a.table + (int64_t)parent * a.max_blocks;
+    int32_t *to = a.table + (int64_t)b * a.max_blocks;
+    bool range = false;
+    for (int j0 = first; j0 < n; j0 += ROW_LOADS * step) {
+        int x[ROW_LOADS];
+#pragma unroll
+        for (int k = 0; k < ROW_LOADS; ++k)
+            x[k] = j0 + k * step < n ? from[j0 + k * step] : 0;
+#pragma unroll
+        for (int k = 0; k < ROW_LOADS; ++k)
+            if (j0 + k * step < n) {
+                to[j0 + k * step] = x[k];
+                if (in_range(x[k], a.n_blocks))
+                    atomicAdd(a.holders + x[k], 1);
+                else
+                    range = true;
+            }
+    }
+    return !range;
+}
+
+// Who becomes whose fork, and the block that it needs for itself: one workgroup, a chunk of 1024 rows at a time.  With `tables` the
+// blocks that are shared as well, a wavefront a row, else they are left to a launch of their own.
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fork_args a, bool tables)
+{
+    __shared__ int length[PQ_PAGED_MAX_SEQS], shares[PQ_PAGED_MAX_SEQS];
     __shared__ scan_room room;
     blocks_scratch &s = *(blocks_scratch *)a.scratch;
     const int most = a.max_blocks << a.log_block, round = (1 << a.log_block) - 1;
@@ -70,7 +97,10 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fo
             a.copy_src[b] = needs && granted ? last : -1;
             a.copy_dst[b] = got;
             a.new_seq_len[b] = granted ? n : length[b];
-            s.shares[b] = granted ? n >> a.log_block : 0;
+            if (tables)
+                shares[b] = granted ? n >> a.log_block : 0;
+            else
+                s.shares[b] = granted ? n >> a.log_block : 0;
             if (granted && part)  // (a number outside the cache stays what it is: nobody follows it)
                 a.table[(int64_t)b * a.max_blocks + (n >> a.log_block)] = needs ? got : last;
             refused |= asks && !granted;
@@ -79,57 +109,116 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fo
     }
     if (threadIdx.x == 0)
         a.new_free_count[0] = count - at_most(before, count);
+    if (tables) {
+        __syncthreads();
+        for (int b = threadIdx.x >> 6; b < a.n_seqs; b += SCAN_WAVES)
+            if (shares[b] > 0)
+                range |= !share_row(a, b, a.parent[b], shares[b], threadIdx.x & 63, 64);
+    }
     if (refused)
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_REFUSED);
     if (range)
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
 }
 
-// The shared blocks into the rows' tables, and counted.  A row that gets blocks was empty: nobody reads it.
 __global__ __launch_bounds__(ROW_THREADS) void pq_paged_fork_tables_kernel(pq_paged_fork_args a)
 {
-    const blocks_scratch &s = *(const blocks_scratch *)a.scratch;
-    const int b = blockIdx.x, n = s.shares[b];
-    if (n == 0)
-        return;
-    const int32_t *from = a.table + (int64_t)a.parent[b] * a.max_blocks;
-    int32_t *to = a.table + (int64_t)b * a.max_blocks;
-    bool range = false;
-    for (int j = blockIdx.y * ROW_THREADS + threadIdx.x; j < n; j += gridDim.y * ROW_THREADS) {
-        const int x = from[j];
-        to[j] = x;
-        if (in_range(x, a.n_blocks))
-            atomicAdd(a.holders + x, 1);
-        else
-            range = true;
-    }
-    if (range)
+    const int b = blockIdx.x, n = ((const blocks_scratch *)a.scratch)->shares[b];
+    if (n > 0 && !share_row(a, b, a.parent[b], n, blockIdx.y * ROW_THREADS + threadIdx.x, gridDim.y * ROW_THREADS))
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
 }
 
 // ---------------------------------------------------------------------------------------------------------- free
+
+__device__ inline int used_blocks(const pq_paged_free_args &a, int b)
+{
+    return (length_of(a.seq_len, b, a.max_blocks << a.log_block) + (1 << a.log_block) - 1) >> a.log_block;
+}
+
+// A row gives its first n blocks back.  What went wrong, as bits of the error word.
+__device__ inline unsigned int release_row(const pq_paged_free_args &a, int b, int n, int first, int step)
+{
+    const int32_t *row = a.table + (int64_t)b * a.max_blocks;
+    unsigned int wrong = 0;
+    for (int j0 = first; j0 < n; j0 += ROW_LOADS * step) {
+        int x[ROW_LOADS], had[ROW_LOADS];
+#pragma unroll
+        for (int k = 0; k < ROW_LOADS; ++k)
+            x[k] = j0 + k * step < n ? row[j0 + k * step] : 0;
+#pragma unroll
+        for (int k = 0; k < ROW_LOADS; ++k) {
+            had[k] = 0;
+            if (j0 + k * step < n) {
+                if (in_range(x[k], a.n_blocks))
+                    had[k] = atomicSub(a.holders + x[k], 1);
+                else
+                    wrong |= PQ_PAGED_ERRFLAG_RANGE;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ROW_LOADS; ++k)
+            if (had[k] < 0) {
+                atomicAdd(a.holders + x[k], 1);
+                wrong |= PQ_PAGED_ERRFLAG_HOLDERS;
+            }
+    }
+    return wrong;
+}
+
+__device__ inline int new_length(const pq_paged_free_args &a, int b)
+{
+    return a.n_new[b] < 0 ? 0 : length_of(a.seq_len, b, a.max_blocks << a.log_block);
+}
 
 __global__ __launch_bounds__(ROW_THREADS) void pq_paged_release_kernel(pq_paged_free_args a)
 {
     const int b = blockIdx.x;
     if (a.n_new[b] >= 0)
         return;
-    const int n = length_of(a.seq_len, b, a.max_blocks << a.log_block), used = (n + (1 << a.log_block) - 1) >> a.log_block;
-    const int32_t *row = a.table + (int64_t)b * a.max_blocks;
-    bool range = false, over = false;
-    for (int j = blockIdx.y * ROW_THREADS + threadIdx.x; j < used; j += gridDim.y * ROW_THREADS) {
-        const int x = row[j];
-        if (!in_range(x, a.n_blocks)) {
-            range = true;
-        } else if (atomicSub(a.holders + x, 1) < 0) {
-            atomicAdd(a.holders + x, 1);
-            over = true;
-        }
+    const unsigned int wrong = release_row(a, b, used_blocks(a, b), blockIdx.y * ROW_THREADS + threadIdx.x, gridDim.y * ROW_THREADS);
+    if (wrong != 0)
+        paged_error(a.dev_err, wrong);
+}
+
+// All of a call whose tables and cache are small, by one workgroup: a wavefront a row, then 16 blocks a thread.
+constexpr int ONE_BLOCKS = 16 * SCAN_THREADS;
+
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_free_kernel(pq_paged_free_args a)
+{
+    __shared__ int gives[PQ_PAGED_MAX_SEQS];
+    __shared__ scan_room room;
+    const int count = between(a.free_count[0], a.n_blocks);
+    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS)
+        gives[b] = a.n_new[b] < 0 ? used_blocks(a, b) : 0;
+    __syncthreads();
+    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS)  // (this thread has read what it may write over)
+        a.new_seq_len[b] = new_length(a, b);
+    unsigned int wrong = 0;
+    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += SCAN_WAVES)
+        if (gives[b] > 0)
+            wrong |= release_row(a, b, gives[b], threadIdx.x & 63, 64);
+    if (wrong != 0)
+        paged_error(a.dev_err, wrong);
+    __threadfence();
+    __syncthreads();
+    // thread 0 has the highest blocks
+    const int each = (a.n_blocks + SCAN_THREADS - 1) / SCAN_THREADS, last = a.n_blocks - 1 - (int)threadIdx.x * each;
+    int goes = 0;
+#pragma unroll
+    for (int k = 0; k < ONE_BLOCKS / SCAN_THREADS; ++k)
+        if (k < each && last - k >= 0)
+            goes |= (__hip_atomic_load(a.holders + last - k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0) << k;
+    int upto = __builtin_popcount(goes), unused = 0, all, all_unused;
+    scan_two(upto, unused, room, all, all_unused);
+    int place = count + upto - __builtin_popcount(goes);
+    for (; goes != 0; goes &= goes - 1, ++place) {
+        const int x = last - __builtin_ctz(goes);
+        a.holders[x] = 0;
+        if (place < a.n_blocks)
+            a.free_list[place] = x;
     }
-    if (range)
-        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
-    if (over)
-        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_HOLDERS);
+    if (threadIdx.x == 0)
+        a.new_free_count[0] = at_most(count + all, a.n_blocks);
 }
 
 // How many numbers of a segment are negative: blocks without a holder (free), free blocks (compact).
@@ -180,7 +269,7 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_push_kernel(pq_paged_fr
         place += found;
     }
     for (int b = blockIdx.x * SCAN_THREADS + threadIdx.x; b < a.n_seqs; b += gridDim.x * SCAN_THREADS)
-        a.new_seq_len[b] = a.n_new[b] < 0 ? 0 : length_of(a.seq_len, b, a.max_blocks << a.log_block);
+        a.new_seq_len[b] = new_length(a, b);
     if (blockIdx.x == 0 && threadIdx.x == 0)
         a.new_free_count[0] = at_most(s.free_count + all, a.n_blocks);
 }
@@ -250,15 +339,125 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_pair_kernel(pq_paged_co
     }
 }
 
-// Tables and counts by the new numbers.  A number that is read while moved_to gets its last values is one or the other,
-// which say the same.
-__global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged_compact_args a, int row_groups)
-{
-    const blocks_scratch &s = *(const blocks_scratch *)a.scratch;
-    const auto moved = [&](int x) {
+// Where a block goes, by moved_to as the kernel above leaves it.  (A number that is read while moved_to gets its last values is one or
+// the other, which say the same.)
+struct by_array {
+    const pq_paged_compact_args &a;
+    int n_live;
+    __device__ by_array(const pq_paged_compact_args &args) : a(args), n_live(((const blocks_scratch *)args.scratch)->n_live) {}
+    __device__ int operator()(int x) const
+    {
         const int v = __hip_atomic_load(a.moved_to + x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         return v < -1 ? a.copy_dst[-2 - v] : v;
-    };
+    }
+    __device__ void told(int, int) const {}
+};
+
+// A cache of up to so many blocks is a bit a block: set where it is free, with the number of set bits in front of each word.  One
+// workgroup makes them in LDS, of the list, and the list of numbers that are taken; all else is worked out from them.
+constexpr int BIT_BLOCKS = 1 << 16, BIT_WORDS = BIT_BLOCKS / 32;
+
+struct bits_scratch {
+    int n_free;
+    unsigned int words[BIT_WORDS];
+    int before[BIT_WORDS];
+};
+
+__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_bits_kernel(pq_paged_compact_args a)
+{
+    __shared__ unsigned int words[BIT_WORDS];
+    __shared__ scan_room room;
+    bits_scratch &s = *(bits_scratch *)a.scratch;
+    const int n_words = (a.n_blocks + 31) / 32;
+    for (int i = threadIdx.x; i < n_words; i += SCAN_THREADS)
+        words[i] = 0;
+    const int count = between(a.free_count[0], a.n_blocks);
+    __syncthreads();
+    bool range = false;
+    constexpr int AT_ONCE = 8;  // loads on their way together
+    for (int i0 = 0; i0 < count; i0 += AT_ONCE * SCAN_THREADS) {
+        int x[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = i0 + k * SCAN_THREADS + (int)threadIdx.x;
+            x[k] = i < count ? a.free_list[i] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (i0 + k * SCAN_THREADS + (int)threadIdx.x < count) {
+                if (in_range(x[k], a.n_blocks))
+                    atomicOr(&words[x[k] >> 5], 1u << (x[k] & 31));
+                else
+                    range = true;
+            }
+    }
+    if (range)
+        paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+    __syncthreads();
+    const int each = (n_words + SCAN_THREADS - 1) / SCAN_THREADS, first = threadIdx.x * each;
+    int found = 0, unused = 0, n_free, all_unused;
+    for (int i = first; i < first + each && i < n_words; ++i)
+        found += __builtin_popcount(words[i]);
+    int upto = found;
+    scan_two(upto, unused, room, n_free, all_unused);
+    const int n_live = a.n_blocks - n_free;
+    int before = upto - found;
+    for (int i = first; i < first + each && i < n_words; ++i) {
+        const unsigned int word = words[i];
+        s.words[i] = word;
+        s.before[i] = before;
+        const int front = n_live - 32 * i;  // of the word, the numbers below n_live
+        unsigned int low = front >= 32 ? word : front <= 0 ? 0u : word & ((1u << front) - 1);
+        if (i == n_live >> 5)
+            a.n_copies[0] = before + __builtin_popcount(low);
+        for (int k = before; low != 0; low &= low - 1, ++k)
+            a.copy_dst[k] = 32 * i + __builtin_ctz(low);
+        before += __builtin_popcount(word);
+    }
+    if (threadIdx.x == 0) {
+        s.n_free = n_free;
+        a.new_free_count[0] = n_free;
+        if (n_live >> 5 >= n_words)  // nothing is free, and the last word is full
+            a.n_copies[0] = 0;
+    }
+}
+
+struct by_bits {
+    const pq_paged_compact_args &a;
+    const bits_scratch &s;
+    int n_live;
+    __device__ by_bits(const pq_paged_compact_args &args)
+        : a(args), s(*(const bits_scratch *)args.scratch), n_live(args.n_blocks - s.n_free)
+    {
+    }
+    // of a live block behind n_live, how many live ones are above it
+    __device__ int from_top(int x) const
+    {
+        const int below = s.before[x >> 5] + __builtin_popcount(s.words[x >> 5] & ((1u << (x & 31)) - 1));
+        return (a.n_blocks - 1 - x) - (s.n_free - below);
+    }
+    __device__ int operator()(int x) const
+    {
+        if (s.words[x >> 5] >> (x & 31) & 1)
+            return -1;
+        return x < n_live ? x : a.copy_dst[from_top(x)];
+    }
+    // what moved_to, the pairs and the new list say of it
+    __device__ void told(int x, int to) const
+    {
+        a.moved_to[x] = to;
+        if (to >= 0 && x >= n_live)
+            a.copy_src[from_top(x)] = x;
+        if (x < s.n_free)
+            a.new_free_list[x] = a.n_blocks - 1 - x;
+    }
+};
+
+// Tables and counts by the new numbers.
+template <typename MOVED>
+__global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged_compact_args a, int row_groups)
+{
+    const MOVED moved(a);
     if ((int)blockIdx.x < a.n_seqs * row_groups) {
         const int b = blockIdx.x / row_groups, group = blockIdx.x - b * row_groups;
         const int n = length_of(a.seq_len, b, a.max_blocks << a.log_block), used = (n + (1 << a.log_block) - 1) >> a.log_block;
@@ -268,25 +467,25 @@ __global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged
             const int x = a.table[at];
             const int to = in_range(x, a.n_blocks) ? moved(x) : x;
             a.new_table[at] = to;
-            range |= to < 0 || !in_range(x, a.n_blocks);
+            range |= !in_range(to, a.n_blocks);
         }
         if (range)
             paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
         return;
     }
     const int groups = gridDim.x - a.n_seqs * row_groups;
-    for (int i = (blockIdx.x - a.n_seqs * row_groups) * ROW_THREADS + threadIdx.x; i < a.n_blocks; i += groups * ROW_THREADS) {
-        const int v = a.moved_to[i];
-        if (i < s.n_live) {
-            if (v >= 0)  // (a free one gets its count from the block that moves there)
-                a.new_holders[i] = a.holders[i];
+    for (int x = (blockIdx.x - a.n_seqs * row_groups) * ROW_THREADS + threadIdx.x; x < a.n_blocks; x += groups * ROW_THREADS) {
+        const int to = moved(x);
+        moved.told(x, to);
+        if (x < moved.n_live) {
+            if (to >= 0)  // (a free one gets its count from the block that moves there)
+                a.new_holders[x] = a.holders[x];
         } else {
-            if (v < -1) {
-                const int to = a.copy_dst[-2 - v];
-                a.new_holders[to] = a.holders[i];
-                __hip_atomic_store(a.moved_to + i, to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            if (to >= 0) {
+                a.new_holders[to] = a.holders[x];
+                __hip_atomic_store(a.moved_to + x, to, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
-            a.new_holders[i] = 0;
+            a.new_holders[x] = 0;
         }
     }
 }
@@ -296,6 +495,10 @@ __global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged
 constexpr int COPY_THREADS = 256;
 constexpr int COPY_LOADS = 4;  // 16-byte loads of a thread on their way together
 constexpr int COPY_UNIT = COPY_THREADS * COPY_LOADS * 16;
+// Workgroups a compute unit, one after another for the most part: with loads and stores that pass the caches 8192 blocks of 64 KiB
+// (1.9 GB moved) take 382 us with 8 of them, 379 with 32, 377 with 64, and 19 000 pairs of a list of 83 000 206, 199 and 195; those that
+// find nothing at the end of a short list cost about a microsecond for each eight.  (Through the caches 388 and 218 us, with 8.)
+constexpr int COPY_PER_CU = 32;
 
 __global__ __launch_bounds__(COPY_THREADS) void pq_paged_copy_kernel(pq_paged_copy_args a)
 {
@@ -319,11 +522,11 @@ __global__ __launch_bounds__(COPY_THREADS) void pq_paged_copy_kernel(pq_paged_co
 #pragma unroll
         for (int i = 0; i < COPY_LOADS; ++i)
             if (at + i * (COPY_THREADS * 16) < a.block_bytes)
-                x[i] = *(const u32x4 *)(from + at + i * (COPY_THREADS * 16));
+                x[i] = __builtin_nontemporal_load((const u32x4 *)(from + at + i * (COPY_THREADS * 16)));
 #pragma unroll
         for (int i = 0; i < COPY_LOADS; ++i)
             if (at + i * (COPY_THREADS * 16) < a.block_bytes)
-                *(u32x4 *)(to + at + i * (COPY_THREADS * 16)) = x[i];
+                __builtin_nontemporal_store(x[i], (u32x4 *)(to + at + i * (COPY_THREADS * 16)));
         if (part == 0)
             for (int h = threadIdx.x; h < a.Hkv; h += COPY_THREADS)
                 a.to_scale[kind][(int64_t)dst * a.Hkv + h] = a.from_scale[kind][(int64_t)src * a.Hkv + h];
@@ -345,17 +548,23 @@ int groups_of_row(int max_blocks)
 
 }  // namespace
 
-int64_t pq_paged_blocks_scratch_bytes() { return sizeof(blocks_scratch); }
+int64_t pq_paged_blocks_scratch_bytes() { return sizeof(bits_scratch) > sizeof(blocks_scratch) ? sizeof(bits_scratch) : sizeof(blocks_scratch); }
 
 hipError_t pq_launch_paged_fork(const pq_paged_fork_args &a, hipStream_t s)
 {
-    hipLaunchKernelGGL(pq_paged_fork_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
-    hipLaunchKernelGGL(pq_paged_fork_tables_kernel, dim3(a.n_seqs, groups_of_row(a.max_blocks)), dim3(ROW_THREADS), 0, s, a);
+    const bool tables = (int64_t)a.n_seqs * a.max_blocks <= ONE_ENTRIES;
+    hipLaunchKernelGGL(pq_paged_fork_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a, tables);
+    if (!tables)
+        hipLaunchKernelGGL(pq_paged_fork_tables_kernel, dim3(a.n_seqs, groups_of_row(a.max_blocks)), dim3(ROW_THREADS), 0, s, a);
     return hipGetLastError();
 }
 
 hipError_t pq_launch_paged_free(const pq_paged_free_args &a, hipStream_t s)
 {
+    if ((int64_t)a.n_seqs * a.max_blocks <= ONE_ENTRIES && a.n_blocks <= ONE_BLOCKS) {
+        hipLaunchKernelGGL(pq_paged_free_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(pq_paged_release_kernel, dim3(a.n_seqs, groups_of_row(a.max_blocks)), dim3(ROW_THREADS), 0, s, a);
     const int n = segments(a.n_blocks), per = per_segment(a.n_blocks);
     hipLaunchKernelGGL(pq_paged_count_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a.holders, a.n_blocks, per, a.scratch, a.free_count);
@@ -365,21 +574,26 @@ hipError_t pq_launch_paged_free(const pq_paged_free_args &a, hipStream_t s)
 
 hipError_t pq_launch_paged_compact(const pq_paged_compact_args &a, hipStream_t s)
 {
-    const int n = segments(a.n_blocks), per = per_segment(a.n_blocks);
-    const int marks = (a.n_blocks + SCAN_THREADS - 1) / SCAN_THREADS;
+    const int rows = groups_of_row(a.max_blocks), others = (a.n_blocks + ROW_THREADS - 1) / ROW_THREADS;
+    const dim3 all(a.n_seqs * rows + (others < 1024 ? others : 1024));
+    if (a.n_blocks <= BIT_BLOCKS) {
+        hipLaunchKernelGGL(pq_paged_bits_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
+        hipLaunchKernelGGL((pq_paged_renumber_kernel<by_bits>), all, dim3(ROW_THREADS), 0, s, a, rows);
+        return hipGetLastError();
+    }
+    const int n = segments(a.n_blocks), per = per_segment(a.n_blocks), marks = (a.n_blocks + SCAN_THREADS - 1) / SCAN_THREADS;
     const dim3 grid(marks < 512 ? marks : 512);
     hipLaunchKernelGGL(pq_paged_mark_kernel, grid, dim3(SCAN_THREADS), 0, s, a, true);
     hipLaunchKernelGGL(pq_paged_mark_kernel, grid, dim3(SCAN_THREADS), 0, s, a, false);
     hipLaunchKernelGGL(pq_paged_count_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a.moved_to, a.n_blocks, per, a.scratch, (const int32_t *)nullptr);
     hipLaunchKernelGGL(pq_paged_pair_kernel, dim3(n), dim3(SCAN_THREADS), 0, s, a, per);
-    const int rows = groups_of_row(a.max_blocks), others = (a.n_blocks + ROW_THREADS - 1) / ROW_THREADS;
-    hipLaunchKernelGGL(pq_paged_renumber_kernel, dim3(a.n_seqs * rows + (others < 1024 ? others : 1024)), dim3(ROW_THREADS), 0, s, a, rows);
+    hipLaunchKernelGGL((pq_paged_renumber_kernel<by_array>), all, dim3(ROW_THREADS), 0, s, a, rows);
     return hipGetLastError();
 }
 
 hipError_t pq_launch_paged_copy(const pq_paged_copy_args &a, int n_cu, hipStream_t s)
 {
-    const int64_t units = (int64_t)a.n_pairs * 2 * ((a.block_bytes + COPY_UNIT - 1) / COPY_UNIT), most = 8 * n_cu;
+    const int64_t units = (int64_t)a.n_pairs * 2 * ((a.block_bytes + COPY_UNIT - 1) / COPY_UNIT), most = COPY_PER_CU * n_cu;
     hipLaunchKernelGGL(pq_paged_copy_kernel, dim3((unsigned)(units < most ? units : most)), dim3(COPY_THREADS), 0, s, a);
     return hipGetLastError();
 }

@@ -241,6 +241,29 @@ def test_compact_any_number_of_blocks(seqs, most, spare, count):
     check_compact(rng, lengths, 16, spare, shared=most // 32 * 16, count=count, change=list_of_all)
 
 
+@pytest.mark.parametrize("n_blocks", [1, 31, 32, 33, 1023, 1024, 4096, 16383, 16384, 16385, 65535, 65536, 65537, 262145])
+def test_caches_around_what_one_workgroup_does(n_blocks):
+    """free and compact of caches that are about as large as their variants take, all kinds of last words and segments."""
+    rng = np.random.default_rng(n_blocks)
+    for spare in sorted({n_blocks, n_blocks // 2, 1, 0}):
+        lengths = [0, (n_blocks - spare) // 3 * 16, 0, 0]
+        lengths[2] = (n_blocks - spare) * 16 - lengths[1]
+        if max(lengths) > 2 ** 24:
+            continue
+        check_compact(rng, lengths, 16, spare, same=spare % 2 == 0)
+        check_free(rng, [1, -1, -1, -1], lengths, 16, spare, same=spare % 2 == 0)
+        check_free(rng, [1, 1, -1, -1], lengths, 16, spare)
+
+
+@pytest.mark.parametrize("seqs,width", [(1, 4095), (1, 4096), (1, 4097), (64, 64), (64, 65), (4096, 1), (4095, 2)])
+def test_tables_around_what_one_workgroup_does(seqs, width):
+    rng = np.random.default_rng(seqs)
+    lengths = np.where(rng.random(seqs) < 0.5, rng.integers(1, width * 16 + 1, seqs), 0)
+    lengths[0] = width * 16
+    check_free(rng, np.where(rng.random(seqs) < 0.6, -1, 1), lengths, 16, 5, shared=min(width, 3) * 16)
+    check_fork(rng, rng.integers(-1, seqs, seqs), rng.integers(0, width * 16 + 1, seqs), lengths, 16, max(1, seqs // 3), width=width)
+
+
 def test_compact_of_lists_and_tables_that_do_not_fit():
     rng = np.random.default_rng(6)
 
