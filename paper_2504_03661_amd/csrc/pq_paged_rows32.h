@@ -119,79 +119,87 @@ template <typename T, int D> struct rows_32 {
         l = 0.0f;
     }
 
+    // The keys from t on: the lane's row attends over those in front of `sees`, and every row over those in front of `whole`
+    __device__ inline void step(const step_bytes<D> &now, int t, int sees, int whole, int half)
+    {
+        f32x16 dot;
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            dot[j] = 0.0f;
+#pragma unroll
+        for (int x = 0; x < D / 16; ++x) {
+            const half8v k = codes8(now.k[x >> 1][2 * (x & 1)], now.k[x >> 1][2 * (x & 1) + 1]);
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i)
+                dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][x], dot, 0, 0, 0);
+        }
+        float s[16];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float by = per_score * now.k_scale[i];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                s[8 * i + j] = fmaf(dot[8 * i + j], by, now.v_log[i]);
+        }
+        if (t + STEP > whole) {
+            asm volatile("");  // (else all steps are masked, without a branch: 48 vector instructions of 277)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (t + 8 * (j >> 2) + 4 * half + (j & 3) >= sees)
+                    s[j] = -INFINITY;
+        }
+        float high = s[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j)
+            high = fmaxf(high, s[j]);
+        if (__ballot(high - base > MOST_BITS) != 0) {
+            high = fmaxf(high, __shfl_xor(high, 32, 64));
+            const float moved = fmaxf(base, weight_base(high)), down = __builtin_amdgcn_exp2f(base - moved);
+            base = moved;
+            l *= down;
+#pragma unroll
+            for (int i = 0; i < DT; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    o[i][j] *= down;
+        }
+        half8v weights[PARTS][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = __builtin_amdgcn_exp2f(s[8 * i + j] - base);
+                sum += x;
+                weights[0][i][j] = (_Float16)x;
+                if (SPLIT)
+                    weights[PARTS - 1][i][j] = (_Float16)(x - (float)weights[0][i][j]);
+            }
+            l = fmaf(sum, now.v_inv[i], l);
+        }
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const half8v v = codes8(now.v[x][0][i], now.v[x][1][i]);
+#pragma unroll
+                for (int j = 0; j < PARTS; ++j)
+                    o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[j][x], o[i], 0, 0, 0);
+            }
+    }
+
     // Keys t0 .. t1 - 1, the first STEP of which are in `now` already.  The lane's row attends over the first `sees` keys of its
-    // sequence, and every row over the first `least`.
+    // sequence, no more than t1, and every row over the first `least`.
     __device__ inline void attend(const pq_paged_view &c, const int32_t *table, block_batch &batch, int last_block, int h, int t0, int t1,
                                   int sees, int least, int lane, step_bytes<D> &now)
     {
-        const int half = lane >> 5;
+        const int half = lane >> 5, whole = least < t1 ? least : t1;
         step_bytes<D> next;
         for (int t = t0; t < t1; t += STEP) {
             const bool more = t + STEP < t1;
             if (more)
                 load_bytes<D>(c, table, batch, last_block, h, t + STEP, lane, next);
-            f32x16 dot;
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                dot[j] = 0.0f;
-#pragma unroll
-            for (int x = 0; x < D / 16; ++x) {
-                const half8v k = codes8(now.k[x >> 1][2 * (x & 1)], now.k[x >> 1][2 * (x & 1) + 1]);
-#pragma unroll
-                for (int i = 0; i < PARTS; ++i)
-                    dot = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[i][x], dot, 0, 0, 0);
-            }
-            float s[16];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float by = per_score * now.k_scale[i];
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    s[8 * i + j] = fmaf(dot[8 * i + j], by, now.v_log[i]);
-            }
-            if (t + STEP > least || t + STEP > t1)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    if (t + 8 * (j >> 2) + 4 * half + (j & 3) >= sees)
-                        s[j] = -INFINITY;
-            float high = s[0];
-#pragma unroll
-            for (int j = 1; j < 16; ++j)
-                high = fmaxf(high, s[j]);
-            if (__ballot(high - base > MOST_BITS) != 0) {
-                high = fmaxf(high, __shfl_xor(high, 32, 64));
-                const float moved = fmaxf(base, weight_base(high)), down = __builtin_amdgcn_exp2f(base - moved);
-                base = moved;
-                l *= down;
-#pragma unroll
-                for (int i = 0; i < DT; ++i)
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        o[i][j] *= down;
-            }
-            half8v weights[PARTS][2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float x = __builtin_amdgcn_exp2f(s[8 * i + j] - base);
-                    sum += x;
-                    weights[0][i][j] = (_Float16)x;
-                    if (SPLIT)
-                        weights[PARTS - 1][i][j] = (_Float16)(x - (float)weights[0][i][j]);
-                }
-                l = fmaf(sum, now.v_inv[i], l);
-            }
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const half8v v = codes8(now.v[x][0][i], now.v[x][1][i]);
-#pragma unroll
-                    for (int j = 0; j < PARTS; ++j)
-                        o[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, weights[j][x], o[i], 0, 0, 0);
-                }
+            step(now, t, sees, whole, half);
             if (more)
                 now = next;
         }

@@ -29,6 +29,9 @@ __device__ inline int steps_of(int keys) { return (keys + STEP - 1) / STEP; }
 
 constexpr int GROUP_ALIGN = WAVES * STEP;
 constexpr int LEAST_STEPS = 2;  // of a range
+// What a step of a group's job counts for beside one of the line: its bytes come from the L2 for all tiles but one (256 sequences of
+// a shared prompt: 1.25 us and 2.45 us, with two wavefronts on a SIMD; 213.0 us where both count alike, 209.7 so).
+constexpr float STEP_OF_GROUP = 0.5f;
 
 // A sequence's place on the line, from the steps that it has: whole shortest ranges, so that in a call that has no more than those
 // none goes from one sequence to the next.
@@ -64,7 +67,7 @@ __device__ inline pq_paged_shared_ranges cut_line(int steps, float group_keys, i
 {
     pq_paged_shared_ranges r;
     const int beside = workgroups - group_jobs;
-    const float all = (float)(WAVES * workgroups), of_job = group_jobs > 0 ? group_keys / (float)(WAVES * STEP * group_jobs) : 0.0f;
+    const float all = (float)(WAVES * workgroups), of_job = group_jobs > 0 ? STEP_OF_GROUP * group_keys / (float)(WAVES * STEP * group_jobs) : 0.0f;
     const float longer = ((float)steps + (float)(WAVES * group_jobs) * of_job) / all, shorter = longer - of_job;
     if (group_jobs > 0 && beside > 0 && shorter >= (float)LEAST_STEPS) {
         r.n_longer = WAVES * beside;
@@ -99,80 +102,105 @@ struct shared_sums {
     int start[PQ_PAGED_MAX_SEQS + 1];        // first position of each group
     int shared[PQ_PAGED_MAX_SEQS];           // tokens that its members share
     int length[PQ_PAGED_MAX_SEQS];           // of the sequence at a position; -1: none
+    int group[PQ_PAGED_MAX_SEQS];            // that the position is in
     int group_jobs[PQ_PAGED_MAX_SEQS + 1];
-    int group_rows[PQ_PAGED_MAX_SEQS];
-    int begin[PQ_PAGED_MAX_SEQS + 1];        // of the sequences that have tokens of their own, on their line
+    int group_rows[PQ_PAGED_MAX_SEQS], group_pieces[PQ_PAGED_MAX_SEQS];
+    int own[PQ_PAGED_MAX_SEQS];              // number of the sequence at a position among those that have tokens of their own; -1: none
+    int begin[PQ_PAGED_MAX_SEQS];            // where such a one begins on the line
 };
 
-// inclusive maximum over the workgroup's threads
-__device__ inline int scan_max(int x, scan_room &room)
+template <int PLAN_WAVES> struct plan_room {
+    int sums[4][PLAN_WAVES];
+    float2 keys[PLAN_WAVES];
+};
+
+// Inclusive sums of four numbers over the workgroup's threads, and their totals.
+template <int PLAN_WAVES> __device__ inline void scan_four(int (&x)[4], int (&all)[4], plan_room<PLAN_WAVES> &room)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        x[k] = lane_scan(x[k]);
+        if (lane == 63)
+            room.sums[k][wave] = x[k];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        all[k] = 0;
+        int before = 0;
+#pragma unroll
+        for (int w = 0; w < PLAN_WAVES; ++w) {
+            const int of_wave = room.sums[k][w];
+            before += w < wave ? of_wave : 0;
+            all[k] += of_wave;
+        }
+        x[k] += before;
+    }
+    __syncthreads();
+}
+
+__device__ inline int running_max(int x, int lane)
+{
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const int y = __shfl_up(x, d, 64);
         x = lane >= d && y > x ? y : x;
     }
-    if (lane == 63)
-        room.wave[0][wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w)
-        x = room.wave[0][w] > x ? room.wave[0][w] : x;
-    __syncthreads();
     return x;
 }
 
-__device__ inline float sum_all(float x, float *room)
+// The plan of a call of more than SMALL_SEQS sequences.  With 256 threads for as many sequences and 1024 for more: 5 us for 256 of
+// them, 7 with 1024 threads, 9 with a scan for each sum.
+template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_paged_shared_plan_kernel(pq_paged_shared_args a)
 {
-    x = wave_sum(x);
-    if ((threadIdx.x & 63) == 0)
-        room[threadIdx.x >> 6] = x;
-    __syncthreads();
-    x = 0.0f;
-    for (int w = 0; w < SCAN_WAVES; ++w)
-        x += room[w];
-    __syncthreads();
-    return x;
-}
-
-__global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_paged_shared_args a)
-{
+    constexpr int PLAN_WAVES = PLAN_THREADS / 64;
     __shared__ shared_sums s;
-    __shared__ scan_room room;
-    __shared__ float float_room[2][SCAN_WAVES];
-    const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G, tiles = own_tiles(G);
+    __shared__ plan_room<PLAN_WAVES> room;
+    const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G, tiles = own_tiles(G), lane = threadIdx.x & 63;
     bool range = false;
-    for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS) {
+    for (int g = threadIdx.x; g <= n_groups; g += PLAN_THREADS) {
+        s.start[g] = between(a.group_start[g], n_seqs);
+        if (g < n_groups)
+            s.shared[g] = a.shared_len[g];
+    }
+    for (int i = threadIdx.x; i < n_seqs; i += PLAN_THREADS) {
         const int b = a.members == nullptr ? i : a.members[i];
         s.length[i] = (unsigned)b < (unsigned)n_seqs ? paged_length(a.c, b) : -2;
     }
+    __syncthreads();
     // where groups begin: as they are given, but never before the one in front
-    int highest = 0;
-    for (int g0 = 0; g0 <= n_groups; g0 += SCAN_THREADS) {
-        const int g = g0 + threadIdx.x;
-        int x = g <= n_groups ? between(a.group_start[g], n_seqs) : 0;
-        x = x > highest ? x : highest;
-        x = scan_max(x, room);
-        if (g <= n_groups)
-            s.start[g] = x;
-        __syncthreads();
-        highest = s.start[g0 + SCAN_THREADS - 1 < n_groups ? g0 + SCAN_THREADS - 1 : n_groups];
+    bool falls = false;
+    for (int g = threadIdx.x; g < n_groups; g += PLAN_THREADS)
+        falls |= s.start[g] > s.start[g + 1];
+    if (__syncthreads_or(falls)) {
+        if (threadIdx.x < 64) {
+            int highest = 0;
+            for (int g0 = 0; g0 <= n_groups; g0 += 64) {
+                int x = g0 + lane <= n_groups ? s.start[g0 + lane] : 0;
+                x = running_max(x > highest ? x : highest, lane);
+                if (g0 + lane <= n_groups)
+                    s.start[g0 + lane] = x;
+                highest = __builtin_amdgcn_readlane(x, 63);
+            }
+        }
         __syncthreads();
     }
-    for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS) {
+    for (int i = threadIdx.x; i < n_seqs; i += PLAN_THREADS) {
         const bool in_group = i >= s.start[0] && i < s.start[n_groups];
         range |= in_group && s.length[i] == -2;
         s.length[i] = in_group && s.length[i] >= 0 ? s.length[i] : -1;
+        s.group[i] = s.length[i] >= 0 ? owner(s.start, n_groups, i) : 0;
     }
     if (range)
         paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
     __syncthreads();
     float of_groups = 0.0f, of_own = 0.0f;
-    for (int g = threadIdx.x; g < n_groups; g += SCAN_THREADS) {
+    for (int g = threadIdx.x; g < n_groups; g += PLAN_THREADS) {
         const int first = s.start[g], n = s.start[g + 1] - first;
         int shared = 0;
         if (n > 1) {
-            shared = a.shared_len[g];
+            shared = s.shared[g];
             shared = shared < s.length[first] ? shared : s.length[first];
             shared = shared > 0 ? shared >> a.c.log_block << a.c.log_block : 0;
         }
@@ -180,76 +208,57 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
         of_groups += (float)group_tiles(n * G) * (float)shared;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n_seqs; i += SCAN_THREADS)
+    for (int i = threadIdx.x; i < n_seqs; i += PLAN_THREADS)
         if (s.length[i] > 0) {
-            const int own = s.length[i] - s.shared[owner(s.start, n_groups, i)];
+            const int own = s.length[i] - s.shared[s.group[i]];
             of_own += own > 0 ? (float)tiles * (float)own : 0.0f;
         }
-    of_groups = sum_all(of_groups, float_room[0]);
-    of_own = sum_all(of_own, float_room[1]);
+    of_groups = wave_sum(of_groups);
+    of_own = wave_sum(of_own);
+    if (lane == 0)
+        room.keys[threadIdx.x >> 6] = make_float2(of_groups, of_own);
+    __syncthreads();
+    of_groups = of_own = 0.0f;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w) {
+        of_groups += room.keys[w].x;
+        of_own += room.keys[w].y;
+    }
     const int most = group_piece(of_groups + of_own, a.workgroups);
 
-    // jobs and rows of partials of the groups
-    int jobs = 0, rows = 0;
-    for (int g0 = 0; g0 < n_groups; g0 += SCAN_THREADS) {
-        const int g = g0 + threadIdx.x;
-        int n = 0, pieces = 0;
-        if (g < n_groups) {
-            n = (s.start[g + 1] - s.start[g]) * G;
-            pieces = pieces_of(s.shared[g], most);
-        }
-        int upto = group_tiles(n) * pieces, upto_rows = n * pieces, all, all_rows;
-        const int mine = upto, mine_rows = upto_rows;
-        scan_two(upto, upto_rows, room, all, all_rows);
-        if (g < n_groups) {
-            s.group_jobs[g] = jobs + upto - mine;
-            s.group_rows[g] = rows + upto_rows - mine_rows;
-        }
-        jobs += all;
-        rows += all_rows;
-    }
-    if (threadIdx.x == 0)
-        s.group_jobs[n_groups] = jobs;
-    __syncthreads();
-    // the line of the sequences' own tokens
-    int line = 0, n_own = 0;
-    for (int i0 = 0; i0 < n_seqs; i0 += SCAN_THREADS) {
+    // jobs and rows of partials of the groups; and the line of the sequences' own tokens
+    int jobs = 0, rows = 0, line = 0, n_own = 0;
+    for (int i0 = 0; i0 < n_seqs; i0 += PLAN_THREADS) {
         const int i = i0 + threadIdx.x;
-        int g = 0, own = 0;
-        if (i < n_seqs && s.length[i] >= 0) {
-            g = owner(s.start, n_groups, i);
-            own = s.length[i] - s.shared[g];
+        int n = 0, pieces = 0, own = 0;
+        if (i < n_groups) {
+            n = (s.start[i + 1] - s.start[i]) * G;
+            pieces = pieces_of(s.shared[i], most);
         }
-        const int steps = own > 0 ? steps_of(own) : 0, place = tiles * place_of(steps);
-        int upto = place, number = steps > 0, all, all_own;
-        scan_two(upto, number, room, all, all_own);
-        const int begin = line + upto - place, at = n_own + number - 1;
+        if (i < n_seqs && s.length[i] >= 0)
+            own = s.length[i] - s.shared[s.group[i]];
+        const int steps = own > 0 ? steps_of(own) : 0;
+        const int mine[4] = {group_tiles(n) * pieces, n * pieces, tiles * place_of(steps), steps > 0};
+        int upto[4] = {mine[0], mine[1], mine[2], mine[3]}, all[4];
+        scan_four(upto, all, room);
+        if (i < n_groups) {
+            s.group_jobs[i] = jobs + upto[0] - mine[0];
+            s.group_rows[i] = rows + upto[1] - mine[1];
+            s.group_pieces[i] = pieces;
+        }
         if (i < n_seqs) {
-            pq_paged_shared_member m;
-            m.b = s.length[i] < 0 ? -1 : a.members == nullptr ? i : a.members[i];
-            m.row = (i - s.start[g]) * G;
-            m.rows = (s.start[g + 1] - s.start[g]) * G;
-            m.group_row = s.group_rows[g];
-            m.group_pieces = m.b < 0 ? 0 : pieces_of(s.shared[g], most);
-            m.own = steps > 0 ? at : -1;
-            m.begin = begin;
-            m.steps = steps;
-            a.w.members[i] = m;
-            if (steps > 0) {
-                pq_paged_shared_own o;
-                o.b = m.b;
-                o.k0 = s.shared[g];
-                o.k1 = s.length[i];
-                o.begin = begin;
-                a.w.own[at] = o;
-                s.begin[at] = begin;
-            }
+            s.own[i] = steps > 0 ? n_own + upto[3] - 1 : -1;
+            if (steps > 0)
+                s.begin[s.own[i]] = line + upto[2] - mine[2];
         }
-        line += all;
-        n_own += all_own;
+        jobs += all[0];
+        rows += all[1];
+        line += all[2];
+        n_own += all[3];
     }
     const pq_paged_shared_ranges ranges = cut_line(line, of_groups, jobs, a.workgroups);
     if (threadIdx.x == 0) {
+        s.group_jobs[n_groups] = jobs;
         pq_paged_shared_head head;
         head.group_jobs = jobs;
         head.group_rows = rows;
@@ -258,13 +267,33 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_shared_plan_kernel(pq_p
         *a.w.head = head;
     }
     __syncthreads();
-    for (int w = threadIdx.x; w < ranges.count; w += SCAN_THREADS)
+    for (int i = threadIdx.x; i < n_seqs; i += PLAN_THREADS) {
+        const int g = s.group[i];
+        pq_paged_shared_member m;
+        m.b = s.length[i] < 0 ? -1 : a.members == nullptr ? i : a.members[i];
+        m.row = (i - s.start[g]) * G;
+        m.rows = (s.start[g + 1] - s.start[g]) * G;
+        m.group_row = s.group_rows[g];
+        m.group_pieces = m.b < 0 ? 0 : s.group_pieces[g];
+        m.own = s.own[i];
+        m.begin = m.own >= 0 ? s.begin[m.own] : 0;
+        m.steps = m.own >= 0 ? steps_of(s.length[i] - s.shared[g]) : 0;
+        a.w.members[i] = m;
+        if (m.own >= 0) {
+            pq_paged_shared_own o;
+            o.b = m.b;
+            o.k0 = s.shared[g];
+            o.k1 = s.length[i];
+            o.begin = m.begin;
+            a.w.own[m.own] = o;
+        }
+    }
+    for (int w = threadIdx.x; w < ranges.count; w += PLAN_THREADS)
         a.w.first[w] = owner(s.begin, n_own, range_begin(ranges, w));
-    for (int e = threadIdx.x; e < jobs; e += SCAN_THREADS) {
+    for (int e = threadIdx.x; e < jobs; e += PLAN_THREADS) {
         const int g = owner(s.group_jobs, n_groups, e);
         pq_paged_shared_job job;
-        group_job(job, s.start[g], (s.start[g + 1] - s.start[g]) * G, s.shared[g], pieces_of(s.shared[g], most), s.group_rows[g],
-                  e - s.group_jobs[g]);
+        group_job(job, s.start[g], (s.start[g + 1] - s.start[g]) * G, s.shared[g], s.group_pieces[g], s.group_rows[g], e - s.group_jobs[g]);
         job.table = a.members == nullptr ? job.table : a.members[job.table];
         a.w.jobs[e] = job;
     }
@@ -279,16 +308,6 @@ struct small_plan {
     pq_paged_shared_head head;
 };
 
-__device__ inline int running_max(int x, int lane)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(x, d, 64);
-        x = lane >= d && y > x ? y : x;
-    }
-    return x;
-}
-
 __device__ inline int of_lane(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 __device__ inline small_plan plan_small(const pq_paged_shared_args &a, int lane)
@@ -299,8 +318,9 @@ __device__ inline small_plan plan_small(const pq_paged_shared_args &a, int lane)
     int lo = is_group ? a.group_start[lane] : 0, hi = is_group ? a.group_start[lane + 1] : 0;
     int asked = is_group ? a.shared_len[lane] : 0;
     p.b = !is_seq ? -1 : a.members == nullptr ? lane : a.members[lane];
+    const int length_of_lane = is_seq ? paged_length(a.c, lane) : -1;  // (asked for at once, and then looked up)
     const bool there = (unsigned)p.b < (unsigned)n_seqs;
-    const int length = there ? paged_length(a.c, p.b) : -1;
+    const int length = __shfl(length_of_lane, p.b & 63, 64);
     lo = running_max(between(lo, n_seqs), lane);
     hi = between(hi, n_seqs);
     hi = hi > lo ? hi : lo;
@@ -506,46 +526,57 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
     if (m.b < 0)
         return;
     const int h = head / a.G, g = head - h * a.G;
-    float top = LOWEST, sum = 0.0f, o[PER_LANE] = {};
-    // `pieces` partials of a row, the first one's row and how many rows they are apart
-    const auto add = [&](int first, int pieces, int stride) {
-        int64_t from = (int64_t)h * a.w.most_rows + first;
-        for (int c0 = 0; c0 < pieces; c0 += 64, from += 64 * (int64_t)stride) {
-            // a lane has a piece's base and sum, and so its weight; one that is not there has the weight 0
-            const int n = pieces - c0 < 64 ? pieces - c0 : 64;
-            const float2 ml = lane < n ? a.w.sums[from + lane * stride] : make_float2(-INFINITY, 0.0f);
-            const float high = fmaxf(top, wave_max(ml.x)), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
-            top = high;
-            sum = fmaf(sum, old, wave_sum(ml.y * by));
-#pragma unroll
-            for (int d = 0; d < PER_LANE; ++d)
-                o[d] *= old;
-            constexpr int AT_ONCE = 8;  // loads on their way together
-            for (int c1 = 0; c1 < n; c1 += AT_ONCE) {
-                float v[AT_ONCE][PER_LANE];
-#pragma unroll
-                for (int c = 0; c < AT_ONCE; ++c)
-#pragma unroll
-                    for (int d = 0; d < PER_LANE; ++d)
-                        v[c][d] = a.w.partials[(from + (c1 + c < n ? c1 + c : 0) * stride) * D + PER_LANE * lane + d];
-#pragma unroll
-                for (int c = 0; c < AT_ONCE; ++c) {
-                    const float weight = lane_of(by, c1 + c);
-#pragma unroll
-                    for (int d = 0; d < PER_LANE; ++d)
-                        o[d] = fmaf(v[c][d], weight, o[d]);
-                }
-            }
-        }
-    };
+    // the row's partials: the group's, then its own, each some rows apart
+    int of_group = 0, group_first = 0, group_stride = 0, of_own = 0, own_first = 0;
     if (m.group_pieces > 0) {
         const int r = m.row + g, row0 = r / GROUP_ROWS * GROUP_ROWS;
-        add(m.group_row + row0 * m.group_pieces + (r - row0), m.group_pieces, m.rows - row0 < GROUP_ROWS ? m.rows - row0 : GROUP_ROWS);
+        of_group = m.group_pieces;
+        group_first = m.group_row + row0 * m.group_pieces + (r - row0);
+        group_stride = m.rows - row0 < GROUP_ROWS ? m.rows - row0 : GROUP_ROWS;
     }
+    const int own_stride = a.G < OWN_ROWS ? a.G : OWN_ROWS;
     if (m.steps > 0) {
-        const int tile = g / OWN_ROWS, begin = m.begin + tile * place_of(m.steps);
-        const int first = range_of(whole.ranges, begin), pieces = range_of(whole.ranges, begin + m.steps - 1) - first + 1;
-        add(own_partial(whole, a.G, m.own * own_tiles(a.G) + tile, first) + g - tile * OWN_ROWS, pieces, a.G < OWN_ROWS ? a.G : OWN_ROWS);
+        const int tile = g / OWN_ROWS, begin = m.begin + tile * place_of(m.steps), first = range_of(whole.ranges, begin);
+        of_own = range_of(whole.ranges, begin + m.steps - 1) - first + 1;
+        own_first = own_partial(whole, a.G, m.own * own_tiles(a.G) + tile, first) + g - tile * OWN_ROWS;
+    }
+    const int pieces = of_group + of_own;
+    const int64_t of_head = (int64_t)h * a.w.most_rows;
+    float top = LOWEST, sum = 0.0f, o[PER_LANE] = {};
+    constexpr int AT_ONCE = 8;  // partials on their way together
+    for (int c0 = 0; c0 < pieces; c0 += 64) {
+        // a lane has a piece's base and sum, and so its weight; one that is not there has the weight 0
+        const int c = c0 + lane, n = pieces - c0 < 64 ? pieces - c0 : 64;
+        const int at = c < of_group ? group_first + c * group_stride : own_first + (c - of_group) * own_stride;
+        const float2 ml = lane < n ? a.w.sums[of_head + at] : make_float2(-INFINITY, 0.0f);
+        float v[AT_ONCE][PER_LANE];
+        const auto ask = [&](int c1) {
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const float *from = a.w.partials + (of_head + of_lane(at, c1 + k < n ? c1 + k : 0)) * D + PER_LANE * lane;
+#pragma unroll
+                for (int d = 0; d < PER_LANE; ++d)
+                    v[k][d] = from[d];
+            }
+        };
+        ask(0);
+        const float high = fmaxf(top, wave_max(ml.x)), old = __builtin_amdgcn_exp2f(top - high), by = __builtin_amdgcn_exp2f(ml.x - high);
+        top = high;
+        sum = fmaf(sum, old, wave_sum(ml.y * by));
+#pragma unroll
+        for (int d = 0; d < PER_LANE; ++d)
+            o[d] *= old;
+        for (int c1 = 0; c1 < n; c1 += AT_ONCE) {
+            if (c1 > 0)
+                ask(c1);
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const float weight = lane_of(by, c1 + k);
+#pragma unroll
+                for (int d = 0; d < PER_LANE; ++d)
+                    o[d] = fmaf(v[k][d], weight, o[d]);
+            }
+        }
     }
     const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
     T *const out = (T *)a.out + ((int64_t)m.b * a.Hq + head) * D + PER_LANE * lane;
@@ -591,8 +622,10 @@ int64_t pq_paged_shared_layout(const pq_paged_ctx *ctx, int n_seqs, int n_groups
 hipError_t pq_launch_paged_shared(const pq_paged_ctx *ctx, const pq_paged_shared_args &a, hipStream_t s)
 {
     const bool small = a.n_seqs <= SMALL_SEQS;
-    if (!small)
-        hipLaunchKernelGGL(pq_paged_shared_plan_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
+    if (!small && a.n_seqs <= 256)
+        hipLaunchKernelGGL((pq_paged_shared_plan_kernel<256>), dim3(1), dim3(256), 0, s, a);
+    else if (!small)
+        hipLaunchKernelGGL((pq_paged_shared_plan_kernel<1024>), dim3(1), dim3(1024), 0, s, a);
     const dim3 grid((unsigned)a.workgroups * (unsigned)a.c.Hkv), rows((unsigned)(((int64_t)a.n_seqs * a.Hq + WAVES - 1) / WAVES));
 #define LAUNCH(T, D)                                                                                \
     do {                                                                                            \
