@@ -311,3 +311,82 @@ def test_refusals_launch_nothing():
         refused(status, pq.pq_paged_shared_decode, h, 3, 2, *args[:i], bad, *args[i + 1:])
     torch.cuda.synchronize()
     assert (out == 7.0).all() and (workspace == 255).all() and pq.pq_paged_device_error(h) == 0
+
+
+def test_many_query_heads_and_many_kv_heads():
+    rng = np.random.default_rng(29)
+    for Hq, Hkv, dim in ((1024, 1, 64), (1024, 1024, 64), (320, 5, 128), (96, 3, 64)):
+        c = Groups(rng, [(64, [64, 70, 150]), (0, [20])], Hkv, dim, 16)
+        ctx = c.context("f16", Hq, Hkv)
+        q, values = queries(rng, c.seqs, Hq, dim, "f16")
+        check(c.call(ctx, q, empty(c, Hq, "f16"), 0.1), *c.expected(values, 0.1), "f16", dim, f"{Hq} {Hkv}")
+
+
+@pytest.mark.parametrize("seqs", [1, 2, 63, 64, 65, 255, 256, 257, 1023, 1024, 1025])
+def test_any_number_of_requests_and_groups(seqs):
+    """Around what a wavefront plans for itself, and what each of the launches that plan takes; groups of all sizes, some empty."""
+    rng = np.random.default_rng(seqs)
+    groups, left = [], seqs
+    while left > 0:
+        m = min(left, int(rng.choice([1, 1, 2, 3, 9, 40])))
+        shared = int(rng.integers(0, 20)) * 16
+        groups.append((shared, [shared + int(n) for n in rng.choice([0, 1, 5, 16, 33, 64, 130], m)]))
+        left -= m
+    for order in (True, False):
+        c = Groups(rng, groups, 2, 64, 16, order=order)
+        ctx = c.context("bf16", 4, 2)
+        q, values = queries(rng, c.seqs, 4, 64, "bf16")
+        out = c.call(ctx, q, empty(c, 4, "bf16"), 0.1, members=order)
+        check(out, *c.expected(values, 0.1), "bf16", 64)
+        assert pq.pq_paged_device_error(ctx.handle) == 0
+
+
+def test_a_call_smaller_than_its_workspace_and_context():
+    rng = np.random.default_rng(30)
+    c = Groups(rng, [(160, [200, 161, 170]), (32, [40, 50])], 2, 128, 16)
+    ctx = context("f16", 8, 2, 128, 16, c.n_blocks, c.width + 100, 300)
+    workspace = work(ctx, 300, 300)
+    q, values = queries(rng, c.seqs, 8, 128, "f16")
+    table = torch.full((5, c.width + 100), -1, dtype=torch.int32, device="cuda")
+    table[:, :c.width] = c.block_table
+    c.block_table = table
+    check(c.call(ctx, q, empty(c, 8, "f16"), 0.1, workspace), *c.expected(values, 0.1), "f16", 128)
+
+
+def test_what_a_row_does_not_see_does_not_reach_it():
+    """NaN in the shared blocks behind a shorter member's length, and in the rows of queries beside it."""
+    rng = np.random.default_rng(31)
+    for dtype in ("f16", "f32"):
+        c = Groups(rng, [(320, [330, 400, 320])], 1, 128, 16, order=False)
+        c.lengths[2] = 100
+        c.seq_len.copy_(dev(c.lengths))
+        ctx = c.context(dtype, 4, 1)
+        q, values = queries(rng, 3, 4, 128, dtype)
+        want = c.expected(values, 0.1)
+        for kind in "kv":
+            c.scale[kind][int(c.table[0, 12])] = float("nan")
+        q[0, :128] = float("nan")
+        out = c.call(ctx, q, empty(c, 4, dtype), 0.1)
+        assert out[:2].isnan().all()
+        check(out[2:], *(x[2:] for x in want), dtype, 128)
+        c.scale["k"][int(c.table[0, 12])] = 0.01
+        c.scale["v"][int(c.table[0, 12])] = 0.01
+        out = c.call(ctx, q, empty(c, 4, dtype), 0.1)
+        assert out[0, 0].isnan().all() and not out[0, 1:].isnan().any() and not out[1:].isnan().any()
+
+
+def test_caches_of_more_than_4_gib():
+    """Blocks at both ends of a cache whose offsets pass 32 bits."""
+    Hkv, dim, block, n = 32, 128, 64, 17_000                   # 256 KiB a block: 4.4 GB each of K and V
+    rng = np.random.default_rng(32)
+    small = Groups(rng, [(128, [200, 300, 129])], Hkv, dim, block)
+    where = np.concatenate([[0, n - 1], rng.choice(np.arange(n - 3000, n - 1), small.n_blocks - 2, replace=False)])
+    ctx = context("f16", Hkv, Hkv, dim, block, n, small.width, 3)
+    for kind in "kv":
+        data = torch.full((n, Hkv, block * dim), 128, dtype=torch.uint8, device="cuda")
+        scale = torch.full((n, Hkv), float("nan"), device="cuda")
+        data[where], scale[where] = small.data[kind], small.scale[kind]
+        small.data[kind], small.scale[kind] = data, scale
+    small.block_table = dev(np.where(small.table >= 0, where[np.clip(small.table, 0, None)], -1))
+    q, values = queries(rng, 3, Hkv, dim, "f16")
+    check(small.call(ctx, q, empty(small, Hkv, "f16"), 0.09), *small.expected(values, 0.09), "f16", dim)
