@@ -142,7 +142,7 @@ template <typename T, int D> struct rows_32 {
                 s[8 * i + j] = fmaf(dot[8 * i + j], by, now.v_log[i]);
         }
         if (t + STEP > whole) {
-            asm volatile("");  // (else all steps are masked, without a branch: 48 vector instructions of 277)
+            asm volatile("");  // (else all steps are masked, without a branch)
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (t + 8 * (j >> 2) + 4 * half + (j & 3) >= sees)
@@ -178,9 +178,9 @@ template <typename T, int D> struct rows_32 {
             l = fmaf(sum, now.v_inv[i], l);
         }
 #pragma unroll
-        for (int i = 0; i < DT; ++i)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
+            for (int i = 0; i < DT; ++i) {
                 const half8v v = codes8(now.v[x][0][i], now.v[x][1][i]);
 #pragma unroll
                 for (int j = 0; j < PARTS; ++j)

@@ -321,23 +321,19 @@ __device__ inline small_plan plan_small(const pq_paged_shared_args &a, int lane)
     const int length_of_lane = is_seq ? paged_length(a.c, lane) : -1;  // (asked for at once, and then looked up)
     const bool there = (unsigned)p.b < (unsigned)n_seqs;
     const int length = __shfl(length_of_lane, p.b & 63, 64);
-    lo = running_max(between(lo, n_seqs), lane);
+    lo = between(lo, n_seqs);
     hi = between(hi, n_seqs);
-    hi = hi > lo ? hi : lo;
+    if (__ballot(is_group && hi < lo) != 0) {  // not ascending: no group begins before the one in front
+        lo = running_max(lo, lane);
+        hi = hi > lo ? hi : lo;
+    }
     p.lo = lo;
     p.rows = is_group ? (hi - lo) * G : 0;
     const int begin = of_lane(lo, 0), end = of_lane(hi, n_groups - 1);
-    // the last group that begins at or before the position, by six halvings
-    int low = 0, high = n_groups;
-#pragma unroll
-    for (int k = 0; k < 6; ++k) {
-        const int mid = (low + high) >> 1, at = __shfl(lo, mid < 63 ? mid : 63, 64);
-        if (high - low > 1) {
-            low = at <= lane ? mid : low;
-            high = at <= lane ? high : mid;
-        }
-    }
-    p.group = low;
+    // the last group that begins at or before the position
+    p.group = 0;
+    for (int g = 1; g < n_groups; ++g)
+        p.group += of_lane(lo, g) <= lane;
     const bool in_group = is_seq && lane >= begin && lane < end;
     p.length = in_group && there ? length : -1;
     if (__ballot(in_group && !there) != 0 && lane == 0)
