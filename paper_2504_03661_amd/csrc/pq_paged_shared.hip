@@ -52,6 +52,17 @@ __device__ inline int group_piece(float keys, int workgroups)
     return (n + GROUP_ALIGN - 1) / GROUP_ALIGN * GROUP_ALIGN;
 }
 
+// Shared tokens that are read by a job of the group, or 0 where that costs more than it saves: a tile's job keeps a workgroup for some
+// microseconds, and what it spares is the reading of the same tokens, from the L2 mostly, by the other members' own tiles.  Even at
+// 128 to 450 tokens spared for each tile: 400 groups of two with 16 shared tokens 54 us so and 81 as jobs, with 128 tokens 92 both, with
+// 256 tokens 133 and 112; 60 groups of eight with 32 tokens 40 and 44, with 128 tokens 52 and 46.
+constexpr int SPARED_KEYS = 256;
+__device__ inline int worth_sharing(int shared, int rows, int G)
+{
+    const int tiles = group_tiles(rows);
+    return (int64_t)shared * (rows / G * own_tiles(G) - tiles) >= (int64_t)SPARED_KEYS * tiles ? shared : 0;
+}
+
 // How many pieces n keys are cut into, none longer than `most`, and their length.  (GROUP_ALIGN divides `most`, so the rounded
 // length is no more than that, and n is behind (pieces - 1) * most: none is empty.)
 __device__ inline int pieces_of(int n, int most) { return (n + most - 1) / most; }
@@ -69,16 +80,19 @@ __device__ inline int range_of(const pq_paged_shared_ranges &r, int step)
 }
 
 // The line's `steps` over the workgroups that the groups' jobs leave: those that run beside them get longer ranges, those that take
-// their place when they are done shorter ones, by what the jobs' wavefronts have to do, so that all end together.
+// their place when they are done shorter ones, by what the jobs' wavefronts have to do, so that all end together.  Where the ones
+// beside them are done with all of it before others could be with a shortest range, there are only those.
 __device__ inline pq_paged_shared_ranges cut_line(int steps, float group_keys, int group_jobs, int workgroups)
 {
     pq_paged_shared_ranges r;
     const int beside = workgroups - group_jobs;
-    const float all = (float)(WAVES * workgroups), of_job = group_jobs > 0 ? STEP_OF_GROUP * group_keys / (float)(WAVES * STEP * group_jobs) : 0.0f;
-    const float longer = ((float)steps + (float)(WAVES * group_jobs) * of_job) / all, shorter = longer - of_job;
-    if (group_jobs > 0 && beside > 0 && shorter >= (float)LEAST_STEPS) {
+    const float of_job = group_jobs > 0 ? STEP_OF_GROUP * group_keys / (float)(WAVES * STEP * group_jobs) : 0.0f;
+    const float least = (float)LEAST_STEPS;
+    if (group_jobs > 0 && beside > 0 && (float)steps > (float)(WAVES * beside) * (of_job + least)) {
+        const float all = (float)(WAVES * workgroups), even = ((float)steps + (float)(WAVES * group_jobs) * of_job) / all - of_job;
+        const float shorter = even > least ? even : least;
         r.n_longer = WAVES * beside;
-        r.longer = (int)(longer * 1.0001f) + 1;
+        r.longer = (int)((shorter + of_job) * 1.0001f) + 1;
         r.shorter = (int)(shorter * 1.0001f) + 1;
     } else {
         const int waves = WAVES * (beside > 0 ? beside : workgroups), each = (steps + waves - 1) / waves;
@@ -209,7 +223,7 @@ template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_p
         if (n > 1) {
             shared = s.shared[g];
             shared = shared < s.length[first] ? shared : s.length[first];
-            shared = shared > 0 ? shared >> a.c.log_block << a.c.log_block : 0;
+            shared = shared > 0 ? worth_sharing(shared >> a.c.log_block << a.c.log_block, n * G, G) : 0;
         }
         s.shared[g] = shared;
         of_groups += (float)group_tiles(n * G) * (float)shared;
@@ -347,7 +361,7 @@ __device__ inline small_plan plan_small(const pq_paged_shared_args &a, int lane)
         paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
     const int of_first = __shfl(p.length, lo < 63 ? lo : 63, 64);
     asked = asked < of_first ? asked : of_first;
-    p.shared = p.rows > G && asked > 0 ? asked >> a.c.log_block << a.c.log_block : 0;
+    p.shared = p.rows > G && asked > 0 ? worth_sharing(asked >> a.c.log_block << a.c.log_block, p.rows, G) : 0;
     const int own = p.length - __shfl(p.shared, p.group, 64);
     const float of_groups = wave_sum((float)group_tiles(p.rows) * (float)p.shared);
     const float of_own = wave_sum(own > 0 ? (float)tiles * (float)own : 0.0f);

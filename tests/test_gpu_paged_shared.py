@@ -85,7 +85,7 @@ def empty(c, Hq, dtype, fill=float("nan")):
 def test_heads_and_types(dtype, Hq, Hkv):
     rng = np.random.default_rng(Hq * 100 + Hkv)
     for dim, block in ((128, 16), (64, 32)):
-        c = Groups(rng, [(64, [64, 100, 301]), (0, [37]), (192, [192, 193]), (32, [0, 32, 1])], Hkv, dim, block)
+        c = Groups(rng, [(64, [64, 100, 301]), (0, [37]), (320, [320, 321, 400, 333]), (192, [192, 193]), (32, [0, 32, 1]), (512, [512, 600])], Hkv, dim, block)
         ctx = c.context(dtype, Hq, Hkv)
         q, values = queries(rng, c.seqs, Hq, dim, dtype, gap=8 * (Hq % 3))
         scale = 1.0 / math.sqrt(dim)
@@ -151,7 +151,7 @@ def test_members_in_order_and_shorter_than_what_is_shared():
 def test_rows_of_no_group_stay_as_they_were():
     """Positions in front of the first group and behind the last, numbers that are no request, groups that are not ascending."""
     rng = np.random.default_rng(21)
-    c = Groups(rng, [(64, [70, 80, 90, 100, 110, 120, 130, 140])], 1, 64, 16, order=False)
+    c = Groups(rng, [(320, [330, 340, 350, 360, 370, 380, 390, 400])], 1, 64, 16, order=False)
     c.groups = [0, 1, 2, 3]
     ctx = c.context("f16", 4, 1)
     q, values = queries(rng, 8, 4, 64, "f16")
@@ -161,7 +161,7 @@ def test_rows_of_no_group_stay_as_they_were():
                                          ([-9, 2, 100, 3, -1], [0, 1, 2, 3, 4, 5, 6, 7], list(range(8)), 0),
                                          ([0, 3, 4, 5, 8], [5, 8, 0, 2 ** 31 - 1, -1, 1, 2, -2 ** 31], [5, 0, 1, 2], 2),
                                          ([3, 3, 3, 3, 3], [0] * 8, [], 0)):
-        c.device_start, c.device_members, c.shared = dev(start), dev(members), dev([64] * 4)
+        c.device_start, c.device_members, c.shared = dev(start), dev(members), dev([320] * 4)
         out = c.call(ctx, q, empty(c, 4, "f16", 7.0), 0.1)
         check(out[inside], *(x[inside] for x in want), "f16", 64)
         assert (out[[b for b in range(8) if b not in inside]] == 7.0).all()
@@ -200,6 +200,17 @@ def test_scores_of_all_sizes(scale):
         ctx = c.context(dtype, 2, 1)
         q, values = queries(rng, c.seqs, 2, 128, dtype)
         check(c.call(ctx, q, empty(c, 2, dtype), scale), *c.expected(values, scale), dtype, 128, dtype)
+
+
+@pytest.mark.parametrize("members,shared", [(2, 240), (2, 256), (3, 128), (3, 112), (9, 32), (9, 16), (17, 16), (18, 16)])
+def test_groups_around_what_is_worth_a_job(members, shared):
+    """Tokens that a group's jobs spare its members, on both sides of what decides whether there are any."""
+    rng = np.random.default_rng(members)
+    for Hq, Hkv in ((4, 4), (6, 1), (16, 1), (20, 1)):
+        c = Groups(rng, [(shared, [shared + 5 * i for i in range(members)]), (0, [7])], Hkv, 64, 16)
+        ctx = c.context("f16", Hq, Hkv)
+        q, values = queries(rng, c.seqs, Hq, 64, "f16")
+        check(c.call(ctx, q, empty(c, Hq, "f16"), 0.1), *c.expected(values, 0.1), "f16", 64, f"{Hq} {Hkv}")
 
 
 def test_many_requests_of_one_token():
@@ -316,7 +327,7 @@ def test_refusals_launch_nothing():
 def test_many_query_heads_and_many_kv_heads():
     rng = np.random.default_rng(29)
     for Hq, Hkv, dim in ((1024, 1, 64), (1024, 1024, 64), (320, 5, 128), (96, 3, 64)):
-        c = Groups(rng, [(64, [64, 70, 150]), (0, [20])], Hkv, dim, 16)
+        c = Groups(rng, [(288, [288, 300, 350]), (64, [64, 70]), (0, [20])], Hkv, dim, 16)
         ctx = c.context("f16", Hq, Hkv)
         q, values = queries(rng, c.seqs, Hq, dim, "f16")
         check(c.call(ctx, q, empty(c, Hq, "f16"), 0.1), *c.expected(values, 0.1), "f16", dim, f"{Hq} {Hkv}")
