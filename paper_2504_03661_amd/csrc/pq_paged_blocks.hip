@@ -18,11 +18,12 @@
 namespace {
 
 constexpr int SEGMENTS = 256;  // of the block numbers, at most, each a workgroup's
-constexpr int ROW_THREADS = 256, ROW_LOADS = 4;  // entries of a thread on their way together
-// Entries of all block tables together up to which one workgroup does a call: with 4000 of them a fork and its copy take 10.3 us, and 13.6
-// with a grid for the tables; an end, behind a copy of the counts, 12.9 and 15.2.  With 16 000 entries it is 18.9 and 13.1, 23.7 and
-// 15.4: all atomics go through one compute unit.
-constexpr int ONE_ENTRIES = 4096;
+constexpr int ROW_THREADS = 256, LOADS = 4;  // entries of a thread on their way together
+// Entries of all block tables together up to which one workgroup does a call, all its threads on all of them: with 4K of them a fork and its
+// copy take 10.3 us, and 13.6 with a grid for the tables; an end, behind a copy of the counts, 10.8 and 15.2; with 7K 11.8 and 13.6,
+// 13.4 and 14.8.  With 8K it is 13.7 and 13.3, 17.2 and 15.1: all atomics go through one compute unit.  (A wavefront a row, 256 requests
+// of 16 blocks: 19.8, 19.4.)
+constexpr int ONE_ENTRIES = 7 * SCAN_THREADS;
 
 // what a call's launches hand over, in the context's scratch
 struct blocks_scratch {
@@ -38,22 +39,25 @@ __device__ inline int length_of(const int32_t *seq_len, int b, int most) { retur
 
 // ---------------------------------------------------------------------------------------------------------- fork
 
-// Row b's shared blocks into its table, and counted, by threads first, first + step, ..  A row that gets blocks was empty: nobody
-// reads it.  Whether all numbers were in range.
-__device__ inline bool share_row(const pq_paged_fork_args &a, int b, int parent, int n, int first, int step)
+// Entries of the tables that become shared, and are counted, by threads first, first + step, .. of n: `from(e)` is where entry e comes from,
+// or -1.  A row that gets blocks was empty: nobody reads it.  Whether all numbers were in range.
+template <typename FROM> __device__ inline bool share(const pq_paged_fork_args &a, int32_t *to, int n, int first, int step, const FROM &from)
 {
-    const int32_t *from = a.table + (int64_t)parent * a.max_blocks;
-    int32_t *to = a.table + (int64_t)b * a.max_blocks;
     bool range = false;
-    for (int j0 = first; j0 < n; j0 += ROW_LOADS * step) {
-        int x[ROW_LOADS];
+    for (int e0 = first; e0 < n; e0 += LOADS * step) {
+        int x[LOADS];
+        bool there[LOADS];
 #pragma unroll
-        for (int k = 0; k < ROW_LOADS; ++k)
-            x[k] = j0 + k * step < n ? from[j0 + k * step] : 0;
+        for (int k = 0; k < LOADS; ++k) {
+            const int e = e0 + k * step;
+            const int64_t at = e < n ? from(e) : -1;
+            there[k] = at >= 0;
+            x[k] = there[k] ? a.table[at] : 0;
+        }
 #pragma unroll
-        for (int k = 0; k < ROW_LOADS; ++k)
-            if (j0 + k * step < n) {
-                to[j0 + k * step] = x[k];
+        for (int k = 0; k < LOADS; ++k)
+            if (there[k]) {
+                to[e0 + k * step] = x[k];
                 if (in_range(x[k], a.n_blocks))
                     atomicAdd(a.holders + x[k], 1);
                 else
@@ -64,10 +68,10 @@ __device__ inline bool share_row(const pq_paged_fork_args &a, int b, int parent,
 }
 
 // Who becomes whose fork, and the block that it needs for itself: one workgroup, a chunk of 1024 rows at a time.  With `tables` the
-// blocks that are shared as well, a wavefront a row, else they are left to a launch of their own.
+// blocks that are shared as well, else they are left to a launch of their own.
 __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fork_args a, bool tables)
 {
-    __shared__ int length[PQ_PAGED_MAX_SEQS], shares[PQ_PAGED_MAX_SEQS];
+    __shared__ int length[PQ_PAGED_MAX_SEQS], shares[PQ_PAGED_MAX_SEQS], parents[PQ_PAGED_MAX_SEQS];
     __shared__ scan_room room;
     blocks_scratch &s = *(blocks_scratch *)a.scratch;
     const int most = a.max_blocks << a.log_block, round = (1 << a.log_block) - 1;
@@ -104,10 +108,12 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fo
             a.copy_src[b] = needs && granted ? last : -1;
             a.copy_dst[b] = got;
             a.new_seq_len[b] = granted ? n : length[b];
-            if (tables)
+            if (tables) {
                 shares[b] = granted ? n >> a.log_block : 0;
-            else
+                parents[b] = p;
+            } else {
                 s.shares[b] = granted ? n >> a.log_block : 0;
+            }
             if (granted && part)  // (a number outside the cache stays what it is: nobody follows it)
                 a.table[(int64_t)b * a.max_blocks + (n >> a.log_block)] = needs ? got : last;
             refused |= asks && !granted;
@@ -118,9 +124,10 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fo
         a.new_free_count[0] = count - at_most(before, count);
     if (tables) {
         __syncthreads();
-        for (int b = threadIdx.x >> 6; b < a.n_seqs; b += SCAN_WAVES)
-            if (shares[b] > 0)
-                range |= !share_row(a, b, a.parent[b], shares[b], threadIdx.x & 63, 64);
+        range |= !share(a, a.table, a.n_seqs * a.max_blocks, threadIdx.x, SCAN_THREADS, [&](int e) {
+            const int b = e / a.max_blocks, j = e - b * a.max_blocks;
+            return j < shares[b] ? parents[b] * a.max_blocks + j : -1;
+        });
     }
     if (refused)
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_REFUSED);
@@ -131,7 +138,11 @@ __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_fork_kernel(pq_paged_fo
 __global__ __launch_bounds__(ROW_THREADS) void pq_paged_fork_tables_kernel(pq_paged_fork_args a)
 {
     const int b = blockIdx.x, n = ((const blocks_scratch *)a.scratch)->shares[b];
-    if (n > 0 && !share_row(a, b, a.parent[b], n, blockIdx.y * ROW_THREADS + threadIdx.x, gridDim.y * ROW_THREADS))
+    if (n <= 0)
+        return;
+    const int64_t parent = (int64_t)a.parent[b] * a.max_blocks;
+    if (!share(a, a.table + (int64_t)b * a.max_blocks, n, blockIdx.y * ROW_THREADS + threadIdx.x, gridDim.y * ROW_THREADS,
+               [&](int j) { return parent + j; }))
         paged_error(a.dev_err, PQ_PAGED_ERRFLAG_RANGE);
 }
 
@@ -142,20 +153,24 @@ __device__ inline int used_blocks(const pq_paged_free_args &a, int b)
     return (length_of(a.seq_len, b, a.max_blocks << a.log_block) + (1 << a.log_block) - 1) >> a.log_block;
 }
 
-// A row gives its first n blocks back.  What went wrong, as bits of the error word.
-__device__ inline unsigned int release_row(const pq_paged_free_args &a, int b, int n, int first, int step)
+// Entries of the tables are given back, by threads first, first + step, .. of n, those for which `is` says so; `freed` hears of blocks that
+// have no holder left.  What went wrong, as bits of the error word.
+template <typename IS, typename FREED>
+__device__ inline unsigned int release(const pq_paged_free_args &a, const int32_t *table, int n, int first, int step, const IS &is, const FREED &freed)
 {
-    const int32_t *row = a.table + (int64_t)b * a.max_blocks;
     unsigned int wrong = 0;
-    for (int j0 = first; j0 < n; j0 += ROW_LOADS * step) {
-        int x[ROW_LOADS], had[ROW_LOADS];
+    for (int e0 = first; e0 < n; e0 += LOADS * step) {
+        int x[LOADS], had[LOADS];
+        bool there[LOADS];
 #pragma unroll
-        for (int k = 0; k < ROW_LOADS; ++k)
-            x[k] = j0 + k * step < n ? row[j0 + k * step] : 0;
+        for (int k = 0; k < LOADS; ++k) {
+            there[k] = e0 + k * step < n && is(e0 + k * step);
+            x[k] = there[k] ? table[e0 + k * step] : 0;
+        }
 #pragma unroll
-        for (int k = 0; k < ROW_LOADS; ++k) {
-            had[k] = 0;
-            if (j0 + k * step < n) {
+        for (int k = 0; k < LOADS; ++k) {
+            had[k] = 1;
+            if (there[k]) {
                 if (in_range(x[k], a.n_blocks))
                     had[k] = atomicSub(a.holders + x[k], 1);
                 else
@@ -163,8 +178,10 @@ __device__ inline unsigned int release_row(const pq_paged_free_args &a, int b, i
             }
         }
 #pragma unroll
-        for (int k = 0; k < ROW_LOADS; ++k)
-            if (had[k] < 0) {
+        for (int k = 0; k < LOADS; ++k)
+            if (had[k] == 0) {
+                freed(x[k]);
+            } else if (had[k] < 0) {
                 atomicAdd(a.holders + x[k], 1);
                 wrong |= PQ_PAGED_ERRFLAG_HOLDERS;
             }
@@ -182,48 +199,51 @@ __global__ __launch_bounds__(ROW_THREADS) void pq_paged_release_kernel(pq_paged_
     const int b = blockIdx.x;
     if (a.n_new[b] >= 0)
         return;
-    const unsigned int wrong = release_row(a, b, used_blocks(a, b), blockIdx.y * ROW_THREADS + threadIdx.x, gridDim.y * ROW_THREADS);
+    const unsigned int wrong = release(a, a.table + (int64_t)b * a.max_blocks, used_blocks(a, b), blockIdx.y * ROW_THREADS + threadIdx.x,
+                                       gridDim.y * ROW_THREADS, [](int) { return true; }, [](int) {});
     if (wrong != 0)
         paged_error(a.dev_err, wrong);
 }
 
-// All of a call whose tables and cache are small, by one workgroup: a wavefront a row, then 16 blocks a thread.
-constexpr int ONE_BLOCKS = 16 * SCAN_THREADS;
+// A cache of up to so many blocks is a bit a block in LDS where one workgroup does the work: of those that are freed, or free.
+constexpr int BIT_BLOCKS = 1 << 16, BIT_WORDS = BIT_BLOCKS / 32;
 
+// All of a call whose tables are small, by one workgroup: all entries, then the words of the freed blocks.
 __global__ __launch_bounds__(SCAN_THREADS) void pq_paged_free_kernel(pq_paged_free_args a)
 {
     __shared__ int gives[PQ_PAGED_MAX_SEQS];
+    __shared__ unsigned int words[BIT_WORDS];
     __shared__ scan_room room;
-    const int count = between(a.free_count[0], a.n_blocks);
-    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS)
+    const int count = between(a.free_count[0], a.n_blocks), n_words = (a.n_blocks + 31) / 32;
+    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS) {
         gives[b] = a.n_new[b] < 0 ? used_blocks(a, b) : 0;
+        a.new_seq_len[b] = new_length(a, b);  // (nobody else reads this sequence's length)
+    }
+    for (int i = threadIdx.x; i < n_words; i += SCAN_THREADS)
+        words[i] = 0;
     __syncthreads();
-    for (int b = threadIdx.x; b < a.n_seqs; b += SCAN_THREADS)  // (this thread has read what it may write over)
-        a.new_seq_len[b] = new_length(a, b);
-    unsigned int wrong = 0;
-    for (int b = threadIdx.x >> 6; b < a.n_seqs; b += SCAN_WAVES)
-        if (gives[b] > 0)
-            wrong |= release_row(a, b, gives[b], threadIdx.x & 63, 64);
+    const auto is = [&](int e) { const int b = e / a.max_blocks; return e - b * a.max_blocks < gives[b]; };
+    const unsigned int wrong = release(a, a.table, a.n_seqs * a.max_blocks, threadIdx.x, SCAN_THREADS, is,
+                                       [&](int x) { atomicOr(&words[x >> 5], 1u << (x & 31)); });
     if (wrong != 0)
         paged_error(a.dev_err, wrong);
-    __threadfence();
     __syncthreads();
     // thread 0 has the highest blocks
-    const int each = (a.n_blocks + SCAN_THREADS - 1) / SCAN_THREADS, last = a.n_blocks - 1 - (int)threadIdx.x * each;
-    int goes = 0;
-#pragma unroll
-    for (int k = 0; k < ONE_BLOCKS / SCAN_THREADS; ++k)
-        if (k < each && last - k >= 0)
-            goes |= (__hip_atomic_load(a.holders + last - k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < 0) << k;
-    int upto = __builtin_popcount(goes), unused = 0, all, all_unused;
+    const int each = (n_words + SCAN_THREADS - 1) / SCAN_THREADS, last = n_words - 1 - (int)threadIdx.x * each;
+    int mine = 0;
+    for (int k = 0; k < each && last - k >= 0; ++k)
+        mine += __builtin_popcount(words[last - k]);
+    int upto = mine, unused = 0, all, all_unused;
     scan_two(upto, unused, room, all, all_unused);
-    int place = count + upto - __builtin_popcount(goes);
-    for (; goes != 0; goes &= goes - 1, ++place) {
-        const int x = last - __builtin_ctz(goes);
-        a.holders[x] = 0;
-        if (place < a.n_blocks)
-            a.free_list[place] = x;
-    }
+    int place = count + upto - mine;
+    for (int k = 0; k < each && last - k >= 0; ++k)
+        for (unsigned int goes = words[last - k]; goes != 0; ++place) {
+            const int at = 31 - __builtin_clz(goes), x = 32 * (last - k) + at;
+            goes ^= 1u << at;
+            a.holders[x] = 0;
+            if (place < a.n_blocks)
+                a.free_list[place] = x;
+        }
     if (threadIdx.x == 0)
         a.new_free_count[0] = at_most(count + all, a.n_blocks);
 }
@@ -360,12 +380,10 @@ struct by_array {
     __device__ void told(int, int) const {}
 };
 
-// A cache of up to so many blocks is a bit a block: set where it is free, with the number of set bits in front of each word.  One
-// workgroup makes them in LDS, of the list, and the list of numbers that are taken; all else is worked out from them.  With the copy
+// Up to BIT_BLOCKS blocks: bits set where they are free, with the number of set bits in front of each word.  One
+// workgroup makes them, of the list, and the list of numbers that are taken; all else is worked out from them.  With the copy
 // 8K blocks take 13.9 us so and 24.6 by the four launches that larger caches need, 33K blocks 24 and 30, 83K blocks 219.6 and 217.2: the
 // one workgroup reads the list alone.
-constexpr int BIT_BLOCKS = 1 << 16, BIT_WORDS = BIT_BLOCKS / 32;
-
 struct bits_scratch {
     int n_free;
     unsigned int words[BIT_WORDS];
@@ -570,7 +588,7 @@ hipError_t pq_launch_paged_fork(const pq_paged_fork_args &a, hipStream_t s)
 
 hipError_t pq_launch_paged_free(const pq_paged_free_args &a, hipStream_t s)
 {
-    if ((int64_t)a.n_seqs * a.max_blocks <= ONE_ENTRIES && a.n_blocks <= ONE_BLOCKS) {
+    if ((int64_t)a.n_seqs * a.max_blocks <= ONE_ENTRIES && a.n_blocks <= BIT_BLOCKS) {
         hipLaunchKernelGGL(pq_paged_free_kernel, dim3(1), dim3(SCAN_THREADS), 0, s, a);
         return hipGetLastError();
     }

@@ -255,7 +255,18 @@ def test_caches_around_what_one_workgroup_does(n_blocks):
         check_free(rng, [1, 1, -1, -1], lengths, 16, spare)
 
 
-@pytest.mark.parametrize("seqs,width", [(1, 4095), (1, 4096), (1, 4097), (64, 64), (64, 65), (4096, 1), (4095, 2)])
+@pytest.mark.parametrize("n_blocks", [64, 4097, 32768, 65535, 65536, 65537])
+def test_few_requests_of_a_large_cache_end(n_blocks):
+    """Small tables, of blocks anywhere among many, the last ones too."""
+    rng = np.random.default_rng(n_blocks)
+    lengths = [400, 100, 0, 33, 300]
+    for n_new in ([-1, -1, -1, -1, -1], [0, -1, -1, 1, -1], [5, 5, 5, 5, 5]):
+        for same in (False, True):
+            check_free(rng, n_new, lengths, 16, n_blocks - 52, shared=32, same=same)
+
+
+@pytest.mark.parametrize("seqs,width", [(1, 4095), (1, 4096), (1, 4097), (64, 64), (64, 65), (4096, 1), (4095, 2), (1, 7168), (1, 7169),
+                                        (64, 112), (64, 113), (1024, 7)])
 def test_tables_around_what_one_workgroup_does(seqs, width):
     rng = np.random.default_rng(seqs)
     lengths = np.where(rng.random(seqs) < 0.5, rng.integers(1, width * 16 + 1, seqs), 0)
