@@ -439,7 +439,9 @@ int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const 
                   const float *from_v_scale, int32_t n_to, uint8_t *to_k, uint8_t *to_v, float *to_k_scale,
                   float *to_v_scale, void *hip_stream);
 
-/* pq_paged_decode for groups of requests that begin with the same blocks: those are read once for a group.
+/* pq_paged_decode for groups of requests that begin with the same blocks: those are read once for a group, unless
+ * that costs more than it saves.  (What shares little and is short by max_blocks takes one launch, other calls two or three: a
+ * call whose requests hold few tokens in wide tables is faster by pq_paged_decode.)
  *
  *   n_groups     1 .. n_seqs (PQ_ERR_SHAPE, PQ_ERR_CAPACITY otherwise); n_seqs * ceil(Hq / Hkv / 16) * max_blocks *
  *                block_tokens < 2^35 (PQ_ERR_CAPACITY)
@@ -447,8 +449,8 @@ int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const 
  *   group_start  device [n_groups + 1] int32  group g is members[group_start[g]] .. members[group_start[g + 1] - 1] (not
  *                ascending: a group that would begin before the one in front of it begins where that does)
  *   shared_len   device [n_groups] int32  tokens that all members of a group begin with, in the same blocks.  What counts is whole
- *                blocks, and no more than the first member has: they are read by its block table.  A member that is shorter attends over
- *                its own length of them
+ *                blocks, and no more than the first member has: they are read by its block table, or by each member's own where that is
+ *                faster.  A member that is shorter attends over its own length of them
  *   workspace    device, 16-byte aligned, at least pq_paged_shared_workspace_bytes(ctx, n_seqs, n_groups) bytes (else
  *                PQ_ERR_CAPACITY); contents need not be initialised.  Calls that may run at the same time need one each
  *   out          device [n_seqs][Hq][d] dtype; rows of requests that are in no group are left as they were

@@ -7,6 +7,8 @@
 // whatever the lengths are, and it goes from one sequence to the next where they end.  Both in one launch, cut so that
 // the chip is filled once; a second one puts every row's pieces together:  with base_i, l_i, o_i of piece i,
 //     m = max base_i,   out = sum 2^(base_i - m) o_i / sum 2^(base_i - m) l_i.
+// Where the block tables are so narrow that a call is short whatever it holds, a workgroup does a sequence's rows of a KV head by itself, in
+// one launch.
 //
 // Long own tokens are bound by HBM (256 chats of a shared prompt of 2048 tokens and 2000 of their own each, 32 query / 8 KV heads, bf16:
 // 207 us, 5.1 TB/s over all; once the groups' jobs are done 6.8 TB/s), many rows over shared ones by the issue of vector and
@@ -620,6 +622,93 @@ __global__ __launch_bounds__(THREADS) void pq_paged_shared_merge_kernel(pq_paged
         out[d] = paged_elem<T>::down(o[d] * by);
 }
 
+// ------------------------------------------------------------------------------------------- calls that can only be small
+
+// A workgroup has a tile of a sequence's rows over all its keys, wherever they come from; its wavefronts share those out and join through LDS.
+// No plan, no partials and no merge; shared tokens are read by each member, from the L2 for the most part.
+template <typename T, int D> __global__ __launch_bounds__(THREADS, 2) void pq_paged_shared_direct_kernel(pq_paged_shared_args a)
+{
+    __shared__ float part[WAVES][OWN_ROWS][D + 4];
+    __shared__ float wave_base[WAVES][OWN_ROWS], wave_l[WAVES][OWN_ROWS];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), col = lane & 15, quad = lane >> 4;
+    const int h = blockIdx.x % a.c.Hkv, unit = blockIdx.x / a.c.Hkv, tiles = own_tiles(a.G);
+    const int i = unit / tiles, row0 = (unit - i * tiles) * OWN_ROWS;
+    const int b = a.members == nullptr ? i : a.members[i], begin = between(a.group_start[0], a.n_seqs);
+    int end = begin;
+    for (int g0 = 1; g0 <= a.n_groups; g0 += 64) {
+        const int start = g0 + lane <= a.n_groups ? between(a.group_start[g0 + lane], a.n_seqs) : 0;
+        end = start > end ? start : end;
+    }
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        const int other = __shfl_xor(end, d, 64);
+        end = other > end ? other : end;
+    }
+    if (i < begin || i >= end)
+        return;
+    if ((unsigned)b >= (unsigned)a.n_seqs) {
+        if (threadIdx.x == 0)
+            paged_error(a.c.dev_err, PQ_PAGED_ERRFLAG_RANGE);
+        return;
+    }
+    const int length = paged_length(a.c, b), share = ((length + WAVES - 1) / WAVES + STEP - 1) / STEP * STEP;
+    const int t0 = wave * share, t1 = t0 + share < length ? t0 + share : length;
+    const int32_t *table = a.c.table + (int64_t)b * a.c.max_blocks;
+    const int rows = a.G - row0 < OWN_ROWS ? a.G - row0 : OWN_ROWS, last_block = (length + (1 << a.c.log_block) - 1) >> a.c.log_block;
+    query_16<T, D> row;
+    load_query((const T *)a.q + (int64_t)b * a.q_stride + (int64_t)(h * a.G + row0 + (col < rows ? col : 0)) * D, quad, row);
+    step_data<D> now;
+    block_batch batch;
+    batch.first = -65;
+    if (t0 < t1)
+        load_step<D>(a.c, table, batch, last_block, h, t0, lane, now);
+    rows_16<T, D> r;
+    r.take(row, a.scale_log2e);
+    r.attend(a.c, table, batch, last_block, h, t0, t1, lane, now);
+    const float l = r.sum();
+    if (quad == 0) {
+        wave_base[wave][col] = r.base;
+        wave_l[wave][col] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+        *(f32x4 *)&part[wave][col][16 * i + 4 * quad] = r.o[i];
+    __syncthreads();
+    T *const out = (T *)a.out + ((int64_t)b * a.Hq + h * a.G + row0) * D;
+    for (int e = threadIdx.x; e < rows * (D / 2); e += THREADS) {
+        const int r = e / (D / 2), d = e % (D / 2) * 2;
+        float top = wave_base[0][r], sum = 0.0f, x = 0.0f, y = 0.0f;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+            top = fmaxf(top, wave_base[w][r]);
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float by = __builtin_amdgcn_exp2f(wave_base[w][r] - top);
+            sum = fmaf(wave_l[w][r], by, sum);
+            x = fmaf(part[w][r][d], by, x);
+            y = fmaf(part[w][r][d + 1], by, y);
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        out[r * D + d] = paged_elem<T>::down(x * by);
+        out[r * D + d + 1] = paged_elem<T>::down(y * by);
+    }
+}
+
+// Where the tables' width says that no call can be larger.  One launch of a few steps against two or three of many: 8 sequences of 1024
+// tokens, 32 query / 8 KV heads, 10.8 us and 13.1, 64 of 256 7.8 and 13.0, 256 of 128 16.1 and 28.3, all of one prompt.  A workgroup gets
+// through 45 GB/s: two sequences of 1280 tokens 11.4 and 12.0, of 1536 12.8 and 11.8 (fp32 1280 13.3 and 12.3), of 4096 29.3 and 13.6.
+// And what is shared is read once for each member: 32 heads, 32 sequences of 512 17.5 and 13.7; of more than SMALL_SEQS, where the
+// other way has a plan to launch, 128 of 512 17.2 and 21.4.  Many workgroups that have little to do cost more than a line of it:
+// 1024 sequences of 32, 46.8 and 38.0.
+constexpr int DIRECT_TOKENS = 1280, DIRECT_UNITS = 2048;
+constexpr int64_t DIRECT_SMALL = 1 << 18, DIRECT_LARGE = 1 << 19;  // tokens of all workgroups
+
+bool is_direct(const pq_paged_shared_args &a)
+{
+    const int64_t width = (int64_t)a.c.max_blocks << a.c.log_block, units = (int64_t)a.n_seqs * own_tiles(a.G) * a.c.Hkv;
+    return width <= DIRECT_TOKENS && units <= DIRECT_UNITS && units * width <= (a.n_seqs <= SMALL_SEQS ? DIRECT_SMALL : DIRECT_LARGE);
+}
+
 constexpr int PER_CU = 2;  // workgroups that run together (with 4, one after another, 32 samples of 8192 tokens 35 us instead of 27)
 
 }  // namespace
@@ -656,6 +745,13 @@ int64_t pq_paged_shared_layout(const pq_paged_ctx *ctx, int n_seqs, int n_groups
 
 hipError_t pq_launch_paged_shared(const pq_paged_ctx *ctx, const pq_paged_shared_args &a, hipStream_t s)
 {
+    if (is_direct(a)) {
+        const dim3 units((unsigned)(a.n_seqs * own_tiles(a.G) * a.c.Hkv));
+#define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_shared_direct_kernel<T, D>), units, dim3(THREADS), 0, s, a)
+        PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);
+#undef LAUNCH
+        return hipGetLastError();
+    }
     const bool small = a.n_seqs <= SMALL_SEQS;
     if (!small && a.n_seqs <= 256)
         hipLaunchKernelGGL((pq_paged_shared_plan_kernel<256>), dim3(1), dim3(256), 0, s, a);

@@ -13,9 +13,17 @@ from tests.test_gpu_paged_attn import queries
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True, params=["narrow", "wide"])
+def tables(request, monkeypatch):
+    """Tables of just the longest request, and such that might hold longer ones: calls that can only be small take another way."""
+    monkeypatch.setattr(Groups, "more", 1280 if request.param == "wide" else 0)
+
+
 class Groups:
     """A cache of random codes and scales, and requests that hold the first blocks of their group's prompt together.  groups:
     for each (shared tokens, [length of each member]).  Blocks that nobody holds have NaN scales: whoever reads one shows it."""
+
+    more = 0                                                   # tokens that a table has room for beyond the longest request's
 
     def __init__(self, rng, groups, Hkv, dim, block, spare=3, order=True):
         self.groups, self.block, self.dim = groups, block, dim
@@ -24,7 +32,7 @@ class Groups:
         rows = rng.permutation(self.seqs) if order else np.arange(self.seqs)
         self.start = np.concatenate([[0], np.cumsum([len(m) for _, m in groups])])
         used = -(-lengths // block)
-        self.width = int(max(1, used.max(initial=1)))
+        self.width = int(max(1, used.max(initial=1))) + self.more // block
         numbers = iter(rng.permutation(int(used.sum()) + sum(s // block for s, _ in groups) + spare))
         table, held = np.full((self.seqs, self.width), -1), set()
         for g, (shared, members) in enumerate(groups):
