@@ -11,7 +11,7 @@
 // one launch.
 //
 // Long own tokens are bound by HBM (256 chats of a shared prompt of 2048 tokens and 2000 of their own each, 32 query / 8 KV heads, bf16:
-// 207 us, 5.1 TB/s over all; once the groups' jobs are done 6.8 TB/s), many rows over shared ones by the issue of vector and
+// 205 us, 5.2 TB/s over all; once the groups' jobs are done 6.8 TB/s), many rows over shared ones by the issue of vector and
 // matrix instructions (512 x 4096 tokens: 60 us, 570 TFLOP/s; vector units busy half of the time, matrix units a fifth), small calls by
 // latency: lengths, block numbers, bytes, and the same again in the merge (9 groups of up to 8 beams, 1000 tokens, fp32 16.7 us; 32 samples
 // of 8192 tokens 24 us; four of 1000 12.2 us, of them 7 the first launch and 3 the second, and 10.5 in one launch).
@@ -26,8 +26,10 @@ namespace {
 
 constexpr int WAVES = JOIN_WAVES, THREADS = 64 * WAVES, STEP = STEP_32;
 constexpr int GROUP_ROWS = JOIN_ROWS, OWN_ROWS = 16;  // of a tile
-constexpr int SMALL_SEQS = 64;                        // a call of up to so many sequences needs no launch that plans it: 1.7 us in every
-                                                      // wavefront instead of 6 and a launch (four samples: 17.0 us with it, 13.1 without)
+// Who plans a call.  Up to SMALL_SEQS sequences every wavefront, with a lane for each: 1.7 us (four samples: 12.0 us, 14.4 where workgroups
+// plan, 17.0 with a launch).  Up to MIDDLE_SEQS every workgroup, a thread each, sums in LDS (256 chats 205.1 us and with a launch 207.4,
+// 128 requests of 500 tokens 18.6 and 21.8, as many of 40 13.6 and 16.8).  For more a launch of one workgroup: 6 to 9 us.
+constexpr int SMALL_SEQS = 64, MIDDLE_SEQS = 256;
 static_assert(STEP_16 == STEP);
 
 __device__ inline int group_tiles(int rows) { return (rows + GROUP_ROWS - 1) / GROUP_ROWS; }
@@ -119,17 +121,17 @@ __device__ inline void group_job(pq_paged_shared_job &job, int first, int rows, 
     job.partial = partial + job.row0 * pieces + piece * job.rows;
 }
 
-// -------------------------------------------------------------------------------------- the plan, by one workgroup
+// -------------------------------------------------------------------------------------- the plan, by a workgroup
 
-struct shared_sums {
-    int start[PQ_PAGED_MAX_SEQS + 1];        // first position of each group
-    int shared[PQ_PAGED_MAX_SEQS];           // tokens that its members share
-    int length[PQ_PAGED_MAX_SEQS];           // of the sequence at a position; -1: none
-    int group[PQ_PAGED_MAX_SEQS];            // that the position is in
-    int group_jobs[PQ_PAGED_MAX_SEQS + 1];
-    int group_rows[PQ_PAGED_MAX_SEQS], group_pieces[PQ_PAGED_MAX_SEQS];
-    int own[PQ_PAGED_MAX_SEQS];              // number of the sequence at a position among those that have tokens of their own; -1: none
-    int begin[PQ_PAGED_MAX_SEQS];            // where such a one begins on the line
+template <int MOST> struct shared_sums {
+    int start[MOST + 1];     // first position of each group
+    int shared[MOST];        // tokens that its members share
+    int length[MOST];        // of the sequence at a position; -1: none
+    int group[MOST];         // that the position is in
+    int group_jobs[MOST + 1];
+    int group_rows[MOST], group_pieces[MOST];
+    int own[MOST];           // number of the sequence at a position among those that have tokens of their own; -1: none
+    int begin[MOST];         // where such a one begins on the line
 };
 
 template <int PLAN_WAVES> struct plan_room {
@@ -173,13 +175,11 @@ __device__ inline int running_max(int x, int lane)
     return x;
 }
 
-// The plan of a call of more than SMALL_SEQS sequences, 256 threads for as many of them and 1024 for more (256 sequences: 5.8 us with
-// 256 threads; 8.4 with 1024 and a scan for each sum).
-template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_paged_shared_plan_kernel(pq_paged_shared_args a)
+// All sums of a call.  Without COMPACT a sequence's number is its position, whether it has tokens of its own or not.
+template <int PLAN_THREADS, int MOST, bool COMPACT>
+__device__ inline pq_paged_shared_head plan_workgroup(const pq_paged_shared_args &a, shared_sums<MOST> &s, plan_room<PLAN_THREADS / 64> &room)
 {
     constexpr int PLAN_WAVES = PLAN_THREADS / 64;
-    __shared__ shared_sums s;
-    __shared__ plan_room<PLAN_WAVES> room;
     const int n_seqs = a.n_seqs, n_groups = a.n_groups, G = a.G, tiles = own_tiles(G), lane = threadIdx.x & 63;
     bool range = false;
     for (int g = threadIdx.x; g <= n_groups; g += PLAN_THREADS) {
@@ -261,7 +261,7 @@ template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_p
         if (i < n_seqs && s.length[i] >= 0)
             own = s.length[i] - s.shared[s.group[i]];
         const int steps = own > 0 ? steps_of(own) : 0;
-        const int mine[4] = {group_tiles(n) * pieces, n * pieces, tiles * place_of(steps), steps > 0};
+        const int mine[4] = {group_tiles(n) * pieces, n * pieces, tiles * place_of(steps), !COMPACT || steps > 0};
         int upto[4] = {mine[0], mine[1], mine[2], mine[3]}, all[4];
         scan_four(upto, all, room);
         if (i < n_groups) {
@@ -270,8 +270,8 @@ template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_p
             s.group_pieces[i] = pieces;
         }
         if (i < n_seqs) {
-            s.own[i] = steps > 0 ? n_own + upto[3] - 1 : -1;
-            if (steps > 0)
+            s.own[i] = mine[3] ? n_own + upto[3] - 1 : -1;
+            if (mine[3])
                 s.begin[s.own[i]] = line + upto[2] - mine[2];
         }
         jobs += all[0];
@@ -279,45 +279,70 @@ template <int PLAN_THREADS> __global__ __launch_bounds__(PLAN_THREADS) void pq_p
         line += all[2];
         n_own += all[3];
     }
-    const pq_paged_shared_ranges ranges = cut_line(line, of_groups, jobs, a.workgroups);
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0)
         s.group_jobs[n_groups] = jobs;
-        pq_paged_shared_head head;
-        head.group_jobs = jobs;
-        head.group_rows = rows;
-        head.n_own = n_own;
-        head.ranges = ranges;
-        *a.w.head = head;
-    }
+    pq_paged_shared_head head;
+    head.group_jobs = jobs;
+    head.group_rows = rows;
+    head.n_own = n_own;
+    head.ranges = cut_line(line, of_groups, jobs, a.workgroups);
     __syncthreads();
-    for (int i = threadIdx.x; i < n_seqs; i += PLAN_THREADS) {
-        const int g = s.group[i];
+    return head;
+}
+
+// For the merge: the head, and where the partials of each position are.
+template <int PLAN_THREADS, int MOST>
+__device__ inline void write_members(const pq_paged_shared_args &a, const shared_sums<MOST> &s, const pq_paged_shared_head &head)
+{
+    if (threadIdx.x == 0)
+        *a.w.head = head;
+    for (int i = threadIdx.x; i < a.n_seqs; i += PLAN_THREADS) {
+        const int g = s.group[i], own = s.length[i] - s.shared[g];
         pq_paged_shared_member m;
         m.b = s.length[i] < 0 ? -1 : a.members == nullptr ? i : a.members[i];
-        m.row = (i - s.start[g]) * G;
-        m.rows = (s.start[g + 1] - s.start[g]) * G;
+        m.row = (i - s.start[g]) * a.G;
+        m.rows = (s.start[g + 1] - s.start[g]) * a.G;
         m.group_row = s.group_rows[g];
         m.group_pieces = m.b < 0 ? 0 : s.group_pieces[g];
         m.own = s.own[i];
         m.begin = m.own >= 0 ? s.begin[m.own] : 0;
-        m.steps = m.own >= 0 ? steps_of(s.length[i] - s.shared[g]) : 0;
+        m.steps = m.b >= 0 && own > 0 ? steps_of(own) : 0;
         a.w.members[i] = m;
-        if (m.own >= 0) {
-            pq_paged_shared_own o;
-            o.b = m.b;
-            o.k0 = s.shared[g];
-            o.k1 = s.length[i];
-            o.begin = m.begin;
-            a.w.own[m.own] = o;
-        }
     }
-    for (int w = threadIdx.x; w < ranges.count; w += PLAN_THREADS)
-        a.w.first[w] = owner(s.begin, n_own, range_begin(ranges, w));
-    for (int e = threadIdx.x; e < jobs; e += PLAN_THREADS) {
-        const int g = owner(s.group_jobs, n_groups, e);
+}
+
+// Job e of the groups' of a plan.
+template <int MOST>
+__device__ inline void plan_job(const pq_paged_shared_args &a, const shared_sums<MOST> &s, int e, pq_paged_shared_job &job)
+{
+    const int g = owner(s.group_jobs, a.n_groups, e);
+    group_job(job, s.start[g], (s.start[g + 1] - s.start[g]) * a.G, s.shared[g], s.group_pieces[g], s.group_rows[g], e - s.group_jobs[g]);
+    job.table = a.members == nullptr ? job.table : a.members[job.table];
+}
+
+// The plan of a call of many sequences.
+constexpr int PLAN_THREADS = SCAN_THREADS;
+
+__global__ __launch_bounds__(PLAN_THREADS) void pq_paged_shared_plan_kernel(pq_paged_shared_args a)
+{
+    __shared__ shared_sums<PQ_PAGED_MAX_SEQS> s;
+    __shared__ plan_room<PLAN_THREADS / 64> room;
+    const pq_paged_shared_head head = plan_workgroup<PLAN_THREADS, PQ_PAGED_MAX_SEQS, true>(a, s, room);
+    write_members<PLAN_THREADS>(a, s, head);
+    for (int i = threadIdx.x; i < a.n_seqs; i += PLAN_THREADS)
+        if (s.own[i] >= 0) {
+            pq_paged_shared_own o;
+            o.b = a.members == nullptr ? i : a.members[i];
+            o.k0 = s.shared[s.group[i]];
+            o.k1 = s.length[i];
+            o.begin = s.begin[s.own[i]];
+            a.w.own[s.own[i]] = o;
+        }
+    for (int w = threadIdx.x; w < head.ranges.count; w += PLAN_THREADS)
+        a.w.first[w] = owner(s.begin, head.n_own, range_begin(head.ranges, w));
+    for (int e = threadIdx.x; e < head.group_jobs; e += PLAN_THREADS) {
         pq_paged_shared_job job;
-        group_job(job, s.start[g], (s.start[g + 1] - s.start[g]) * G, s.shared[g], s.group_pieces[g], s.group_rows[g], e - s.group_jobs[g]);
-        job.table = a.members == nullptr ? job.table : a.members[job.table];
+        plan_job(a, s, e, job);
         a.w.jobs[e] = job;
     }
 }
@@ -446,10 +471,23 @@ __device__ inline void attend_range(const pq_paged_shared_args &a, const pq_page
     }
 }
 
-template <typename T, int D, bool SMALL>
+// Who plans: every wavefront, every workgroup, or a launch before this one
+enum { BY_WAVE, BY_WORKGROUP, BY_LAUNCH };
+
+template <int BY> struct planned {};
+template <> struct planned<BY_WORKGROUP> {
+    shared_sums<MIDDLE_SEQS> s;
+    plan_room<WAVES> room;
+};
+
+__device__ inline void make_uniform(int &x) { x = __builtin_amdgcn_readfirstlane(x); }
+
+template <typename T, int D, int BY>
 __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shared_kernel(pq_paged_shared_args a)
 {
+    constexpr bool SMALL = BY == BY_WAVE;
     __shared__ join_room<D> room;
+    __shared__ planned<BY> plan;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv;
     small_plan p;
@@ -464,6 +502,16 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shar
             if (lane == 0)
                 *a.w.head = p.head;
         }
+    } else if constexpr (BY == BY_WORKGROUP) {
+        p.head = plan_workgroup<THREADS, MIDDLE_SEQS, false>(a, plan.s, plan.room);
+        make_uniform(p.head.group_jobs);
+        make_uniform(p.head.group_rows);
+        make_uniform(p.head.ranges.n_longer);
+        make_uniform(p.head.ranges.longer);
+        make_uniform(p.head.ranges.shorter);
+        make_uniform(p.head.ranges.count);
+        if (blockIdx.x == 0)
+            write_members<THREADS>(a, plan.s, p.head);
     } else {
         p.head = *a.w.head;
     }
@@ -483,6 +531,22 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shar
                     const int i = __builtin_ctzll(mine);
                     attend_range<T, D>(a, p.head, h, lane, range, of_lane(p.b, i), of_lane(shared, i), of_lane(p.length, i),
                                        of_lane(p.begin, i), i);
+                }
+            } else if constexpr (BY == BY_WORKGROUP) {
+                const int tiles = own_tiles(a.G);
+                for (int step = range_begin(p.head.ranges, range); step < end;) {
+                    int i = owner(plan.s.begin, a.n_seqs, step);  // (the last of those that begin there: it has tokens of its own)
+                    make_uniform(i);
+                    int b = a.members == nullptr ? i : a.members[i], k0 = plan.s.shared[plan.s.group[i]], k1 = plan.s.length[i], begin = plan.s.begin[i];
+                    make_uniform(b);
+                    make_uniform(k0);
+                    make_uniform(k1);
+                    make_uniform(begin);
+                    const int after = k1 > k0 ? begin + tiles * place_of(steps_of(k1 - k0)) : step;
+                    if (after <= step)  // (the last range may end behind the line)
+                        break;
+                    attend_range<T, D>(a, p.head, h, lane, range, b, k0, k1, begin, i);
+                    step = after;
                 }
             } else {
                 int i = a.w.first[range];
@@ -510,7 +574,18 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shar
             length = __shfl(p.length, job.position + at, 64);
             job.table = of_lane(p.b, job.table);
         } else {
-            job = a.w.jobs[e];
+            if constexpr (BY == BY_WORKGROUP) {
+                plan_job(a, plan.s, e, job);
+                make_uniform(job.table);
+                make_uniform(job.position);
+                make_uniform(job.row0);
+                make_uniform(job.rows);
+                make_uniform(job.k0);
+                make_uniform(job.k1);
+                make_uniform(job.partial);
+            } else {
+                job = a.w.jobs[e];
+            }
             row = job.row0 + (col < job.rows ? col : 0);
             at = row / a.G;
             b = a.members == nullptr ? job.position + at : a.members[job.position + at];
@@ -695,10 +770,10 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS, 2) void pq_pa
 }
 
 // Where the tables' width says that no call can be larger.  One launch of a few steps against two or three of many: 8 sequences of 1024
-// tokens, 32 query / 8 KV heads, 10.8 us and 13.1, 64 of 256 7.8 and 13.0, 256 of 128 16.1 and 28.3, all of one prompt.  A workgroup gets
+// tokens, 32 query / 8 KV heads, 10.8 us and 13.1, 64 of 256 7.8 and 13.0, 256 of 256 20.4 and 26.9, all of one prompt.  A workgroup gets
 // through 45 GB/s: two sequences of 1280 tokens 11.4 and 12.0, of 1536 12.8 and 11.8 (fp32 1280 13.3 and 12.3), of 4096 29.3 and 13.6.
 // And what is shared is read once for each member: 32 heads, 32 sequences of 512 17.5 and 13.7; of more than SMALL_SEQS, where the
-// other way has a plan to launch, 128 of 512 17.2 and 21.4.  Many workgroups that have little to do cost more than a line of it:
+// other way's plan takes longer, 128 of 512 17.2 and 18.6.  Many workgroups that have little to do cost more than a line of it:
 // 1024 sequences of 32, 46.8 and 38.0.
 constexpr int DIRECT_TOKENS = 1280, DIRECT_UNITS = 2048;
 constexpr int64_t DIRECT_SMALL = 1 << 18, DIRECT_LARGE = 1 << 19;  // tokens of all workgroups
@@ -752,18 +827,17 @@ hipError_t pq_launch_paged_shared(const pq_paged_ctx *ctx, const pq_paged_shared
 #undef LAUNCH
         return hipGetLastError();
     }
-    const bool small = a.n_seqs <= SMALL_SEQS;
-    if (!small && a.n_seqs <= 256)
-        hipLaunchKernelGGL((pq_paged_shared_plan_kernel<256>), dim3(1), dim3(256), 0, s, a);
-    else if (!small)
-        hipLaunchKernelGGL((pq_paged_shared_plan_kernel<1024>), dim3(1), dim3(1024), 0, s, a);
+    if (a.n_seqs > MIDDLE_SEQS)
+        hipLaunchKernelGGL(pq_paged_shared_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, s, a);
     const dim3 grid((unsigned)a.workgroups * (unsigned)a.c.Hkv), rows((unsigned)(((int64_t)a.n_seqs * a.Hq + WAVES - 1) / WAVES));
 #define LAUNCH(T, D)                                                                                \
     do {                                                                                            \
-        if (small)                                                                                  \
-            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, true>), grid, dim3(THREADS), 0, s, a);  \
-        else                                                                                        \
-            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, false>), grid, dim3(THREADS), 0, s, a); \
+        if (a.n_seqs <= SMALL_SEQS)                                                                        \
+            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, BY_WAVE>), grid, dim3(THREADS), 0, s, a);      \
+        else if (a.n_seqs <= MIDDLE_SEQS)                                                                  \
+            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, BY_WORKGROUP>), grid, dim3(THREADS), 0, s, a); \
+        else                                                                                               \
+            hipLaunchKernelGGL((pq_paged_shared_kernel<T, D, BY_LAUNCH>), grid, dim3(THREADS), 0, s, a);    \
         hipLaunchKernelGGL((pq_paged_shared_merge_kernel<T, D>), rows, dim3(THREADS), 0, s, a);      \
     } while (0)
     PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);

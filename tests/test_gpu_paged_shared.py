@@ -176,6 +176,31 @@ def test_rows_of_no_group_stay_as_they_were():
         assert pq.pq_paged_device_error(ctx.handle) == told
 
 
+@pytest.mark.parametrize("seqs", [60, 100, 256, 300])
+def test_groups_of_many_that_leave_some_out(seqs):
+    """The same in calls that are planned in each of the ways: a group begins where it says, or where one in front of it does."""
+    rng = np.random.default_rng(seqs)
+    c = Groups(rng, [(160, [160 + int(n) for n in rng.choice([0, 0, 0, 1, 40, 100], seqs)])], 1, 64, 16, order=False)
+    n_groups = seqs // 5
+    c.groups = list(range(n_groups))
+    ctx = c.context("f16", 4, 1)
+    q, values = queries(rng, seqs, 4, 64, "f16")
+    want = c.expected(values, 0.1)
+    for bad in (False, True):
+        start = np.sort(rng.integers(3, seqs - 4, n_groups + 1))
+        start[rng.integers(1, n_groups, 4)] = rng.integers(-5, seqs // 2, 4)
+        members = rng.permutation(seqs)
+        if bad:
+            members[rng.integers(0, seqs, 5)] = [-1, seqs, 2 ** 31 - 1, -2 ** 31, seqs + 7]
+        placed = members[max(start[0], 0):np.clip(start.max(), 0, seqs)]
+        inside = placed[(placed >= 0) & (placed < seqs)].tolist()
+        c.device_start, c.device_members, c.shared = dev(start), dev(members), dev(np.minimum(rng.integers(-20, 400, n_groups), 160))
+        out = c.call(ctx, q, empty(c, 4, "f16", 7.0), 0.1)
+        check(out[inside], *(x[inside] for x in want), "f16", 64)
+        assert (out[[b for b in range(seqs) if b not in inside]] == 7.0).all()
+        assert pq.pq_paged_device_error(ctx.handle) == (2 if len(inside) < len(placed) else 0)
+
+
 def test_blocks_that_are_not_there_and_values_that_are_no_numbers():
     """A block outside the cache counts as no tokens, for all that would read it; NaN scales reach those that read them, no others."""
     rng = np.random.default_rng(22)
