@@ -303,6 +303,38 @@ def test_a_graph_follows_lengths_groups_and_tables():
         assert torch.equal(again, out)
 
 
+@pytest.mark.parametrize("seqs", [20, 100, 300])
+def test_graphs_of_one_workspace(seqs):
+    """Two graphs that work in the same bytes, one after another, with lengths that change; each kind of plan."""
+    rng = np.random.default_rng(seqs)
+    groups = [(int(s) * 16, [int(s) * 16 + int(n) for n in rng.integers(0, 70, 5)]) for s in rng.integers(0, 30, seqs // 5)]
+    cases, n = [], 0
+    for _ in range(2):
+        c = Groups(rng, groups, 2, 64, 16)
+        ctx = c.context("bf16", 8, 2)
+        q, values = queries(rng, c.seqs, 8, 64, "bf16")
+        n = max(n, pq.pq_paged_shared_workspace_bytes(ctx.handle, c.seqs, len(groups)))
+        cases.append([c, ctx, q, values, empty(c, 8, "bf16"), torch.cuda.CUDAGraph()])
+    workspace = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    for c, ctx, q, _, out, graph in cases:
+        c.call(ctx, q, out, 0.1, workspace)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            c.call(ctx, q, out, 0.1, workspace)
+    for step in range(4):
+        for c, ctx, _, _, out, _ in cases:
+            out.fill_(7.0)
+            if step:
+                c.lengths = np.minimum(c.lengths, rng.integers(0, 600, c.seqs))
+                c.seq_len.copy_(dev(c.lengths))
+        for *_, graph in cases:
+            graph.replay()
+        torch.cuda.synchronize()
+        for c, ctx, _, values, out, _ in cases:
+            check(out, *c.expected(values, 0.1), "bf16", 64, f"replay {step}")
+            assert pq.pq_paged_device_error(ctx.handle) == 0
+
+
 def test_two_calls_at_once_with_a_workspace_each():
     rng = np.random.default_rng(27)
     c = Groups(rng, [(6000 // 16 * 16, [6100 + i for i in range(12)])], 2, 128, 16)
