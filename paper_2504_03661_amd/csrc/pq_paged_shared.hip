@@ -26,6 +26,9 @@ namespace {
 
 constexpr int WAVES = JOIN_WAVES, THREADS = 64 * WAVES, STEP = STEP_32;
 constexpr int GROUP_ROWS = JOIN_ROWS, OWN_ROWS = 16;  // of a tile
+// Workgroups of a compute unit that run together: what the kernel's registers and LDS leave room for, in every type and size (with 4, one after
+// another, 32 samples of 8192 tokens 35 us instead of 27).
+constexpr int PER_CU = 2;
 // Who plans a call.  Up to SMALL_SEQS sequences every wavefront, with a lane for each: 1.7 us (four samples: 12.0 us, 14.4 where workgroups
 // plan, 17.0 with a launch).  Up to MIDDLE_SEQS every workgroup, a thread each, sums in LDS (256 chats 205.1 us and with a launch 207.4,
 // 128 requests of 500 tokens 18.6 and 21.8, as many of 40 13.6 and 16.8).  For more a launch of one workgroup: 6 to 9 us.
@@ -483,15 +486,16 @@ template <> struct planned<BY_WORKGROUP> {
 __device__ inline void make_uniform(int &x) { x = __builtin_amdgcn_readfirstlane(x); }
 
 template <typename T, int D, int BY>
-__global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shared_kernel(pq_paged_shared_args a)
+__global__ __launch_bounds__(THREADS, PER_CU) void pq_paged_shared_kernel(pq_paged_shared_args a)
 {
     constexpr bool SMALL = BY == BY_WAVE;
     __shared__ join_room<D> room;
     __shared__ planned<BY> plan;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int of_thread = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int h = blockIdx.x % a.c.Hkv;
     small_plan p;
     if constexpr (SMALL) {
+        const int lane = of_thread;
         p = plan_small(a, lane);
         if (blockIdx.x == 0 && wave == 0) {  // for the merge
             const int lo = __shfl(p.lo, p.group, 64), rows = __shfl(p.rows, p.group, 64);
@@ -518,6 +522,8 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shar
     // The groups' jobs first, then four ranges of the line at a time; the grid is what runs together
     const int stride = gridDim.x / a.c.Hkv, jobs = p.head.group_jobs + (p.head.ranges.count + WAVES - 1) / WAVES;
     for (int e = blockIdx.x / a.c.Hkv; e < jobs; e += stride) {
+        int lane = of_thread;
+        work_out_here<T, D>(lane);
         if (e >= p.head.group_jobs) {
             const int range = (e - p.head.group_jobs) * WAVES + wave;
             if (range >= p.head.ranges.count)
@@ -611,7 +617,9 @@ __global__ __launch_bounds__(THREADS, sizeof(T) == 4 ? 1 : 2) void pq_paged_shar
         r.attend(a.c, table, batch, last_block, h, t0, t1, sees, least, lane, now);
         room.join(r, wave, lane);
         const int64_t to = (int64_t)h * a.w.most_rows + job.partial;
-        for (int i = threadIdx.x; i < job.rows * (D / 2); i += THREADS) {
+        int thread = threadIdx.x;
+        work_out_here<T, D>(thread);
+        for (int i = thread; i < job.rows * (D / 2); i += THREADS) {
             const int r = i / (D / 2), d = i % (D / 2) * 2;
             *(float2 *)(a.w.partials + (to + r) * D + d) = room.values(r, d);
             if (d == 0)
@@ -783,8 +791,6 @@ bool is_direct(const pq_paged_shared_args &a)
     const int64_t width = (int64_t)a.c.max_blocks << a.c.log_block, units = (int64_t)a.n_seqs * own_tiles(a.G) * a.c.Hkv;
     return width <= DIRECT_TOKENS && units <= DIRECT_UNITS && units * width <= (a.n_seqs <= SMALL_SEQS ? DIRECT_SMALL : DIRECT_LARGE);
 }
-
-constexpr int PER_CU = 2;  // workgroups that run together (with 4, one after another, 32 samples of 8192 tokens 35 us instead of 27)
 
 }  // namespace
 

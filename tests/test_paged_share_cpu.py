@@ -11,7 +11,7 @@ import pytest
 import paper_2504_03661_amd as P
 from oracle import paged_oracle as O
 from paper_2504_03661_amd import binding as B
-from tests.test_exchange_codegen_cpu import assembly
+from tests.test_exchange_codegen_cpu import assembly, kernels
 from tests.test_paged_boundary_cpu import HIGH, SAMPLES, Tensor
 
 NAMES = ("fork", "free", "compact", "copy", "shared_decode")
@@ -98,3 +98,21 @@ def test_no_kernel_spills(source, tmp_path):
     assert spills
     for name, n in spills.items():
         assert n <= (8 if "If" in name else 0), (name, n)
+
+
+def test_two_workgroups_of_shared_decode_fit_a_compute_unit(tmp_path):
+    """What its grid and the cut of its work are made for: 256 of a SIMD's 512 registers a wavefront, half of 160 KB a workgroup.  And
+    what is spilled to keep to that is not read in the loops over keys."""
+    text = assembly("pq_paged_shared.hip", tmp_path)
+    entries = {re.search(r"\.name:\s+(\S+)", e).group(1): e for e in re.findall(r"  - \.agpr_count.*?\.wavefront_size", text, re.S)}
+    names = [k for k in entries if "pq_paged_shared_kernel" in k]
+    assert len(names) == 3 * 2 * 3                              # types, dims, who plans
+    bodies = kernels(text)
+    for name in names:
+        registers, lds, spilled = (int(re.search(rf"\.{field}:\s+(\d+)", entries[name]).group(1))
+                                   for field in ("vgpr_count", "group_segment_fixed_size", "vgpr_spill_count"))
+        assert registers <= 256 and lds <= 80 * 1024, (name, registers, lds)
+        assert spilled <= (2 if "IfLi128" in name else 0), (name, spilled)
+        parts = re.split(r"^(?=\.LBB)", bodies[name], flags=re.M)
+        products = [part for part in parts if "v_mfma" in part]
+        assert products and not any("scratch_" in part for part in products), name
