@@ -466,3 +466,37 @@ def test_caches_of_more_than_4_gib():
     small.block_table = dev(np.where(small.table >= 0, where[np.clip(small.table, 0, None)], -1))
     q, values = queries(rng, 3, Hkv, dim, "f16")
     check(small.call(ctx, q, empty(small, Hkv, "f16"), 0.09), *small.expected(values, 0.09), "f16", dim)
+
+
+@pytest.mark.parametrize("seqs", [65, 256, 257, 1025])
+@pytest.mark.parametrize("dtype,dim,Hq,Hkv", [("f32", 128, 4, 2), ("f32", 64, 3, 1), ("f16", 128, 8, 2), ("bf16", 128, 4, 4), ("f32", 128, 33, 1),
+                                              ("f16", 64, 40, 2), ("bf16", 64, 49, 1), ("f32", 64, 40, 2)])
+def test_large_calls_of_every_type_and_of_many_heads(dtype, dim, Hq, Hkv, seqs):
+    """Calls that workgroups plan, and such that a launch plans: every type and size, and heads that take two to four tiles of rows, so that
+    ranges of the line begin and end in any of them."""
+    rng = np.random.default_rng(seqs * 1000 + Hq * 10 + Hkv)
+    groups, left = [], seqs
+    while left > 0:
+        m = min(left, int(rng.choice([1, 2, 3, 9, 40])))
+        shared = int(rng.choice([0, 16, 64, 160, 320]))
+        groups.append((shared, [shared + int(n) for n in rng.choice([0, 1, 5, 33, 64, 65, 130, 300], m, p=[.1, .2, .2, .1, .1, .1, .1, .1])]))
+        left -= m
+    c = Groups(rng, groups, Hkv, dim, 16)
+    ctx = c.context(dtype, Hq, Hkv)
+    q, values = queries(rng, c.seqs, Hq, dim, dtype)
+    first = c.call(ctx, q, empty(c, Hq, dtype), 0.09)
+    check(first, *c.expected(values, 0.09), dtype, dim)
+    assert torch.equal(c.call(ctx, q, empty(c, Hq, dtype), 0.09), first)          # bit for bit
+    assert pq.pq_paged_device_error(ctx.handle) == 0
+
+
+@pytest.mark.parametrize("seqs", [3, 70, 300])
+def test_full_precision_of_long_prompts_and_chats(seqs):
+    """fp32, 128 dims: groups' jobs in several pieces and long ranges of the line in one call, by each kind of plan."""
+    rng = np.random.default_rng(seqs)
+    groups = [(2048, [2048 + int(n) for n in rng.integers(0, 200, 2)]), (0, [1500])]
+    groups += [(96, [96 + int(n) for n in rng.integers(0, 90, m)]) for m in (seqs - 3 - (seqs - 3) // 2, (seqs - 3) // 2) if m]
+    c = Groups(rng, groups, 2, 128, 16)
+    ctx = c.context("f32", 8, 2)
+    q, values = queries(rng, c.seqs, 8, 128, "f32")
+    check(c.call(ctx, q, empty(c, 8, "f32"), 0.09), *c.expected(values, 0.09), "f32", 128)
