@@ -779,17 +779,21 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS, 2) void pq_pa
 
 // Where the tables' width says that no call can be larger.  One launch of a few steps against two or three of many: 8 sequences of 1024
 // tokens, 32 query / 8 KV heads, 10.8 us and 13.1, 64 of 256 7.8 and 13.0, 256 of 256 20.4 and 26.9, all of one prompt.  A workgroup gets
-// through 45 GB/s: two sequences of 1280 tokens 11.4 and 12.0, of 1536 12.8 and 11.8 (fp32 1280 13.3 and 12.3), of 4096 29.3 and 13.6.
+// through 45 GB/s: two sequences of 1280 tokens 11.4 and 12.0, of 1536 12.8 and 11.8, of 4096 29.3 and 13.6; fewer in fp32 with 128 dims,
+// where the other way takes longer only for more sequences: of 1264 tokens one 13.0 and 12.0, two 13.1 and 12.4, four 13.2 and 13.0, eight
+// 13.2 and 14.4; of 1136 one 12.2 and 12.0, two 12.3 both, four 12.3 and 13.1 (64 dims, 1264: one 9.6 and 9.9, two 9.6 and 10.1).
 // And what is shared is read once for each member: 32 heads, 32 sequences of 512 17.5 and 13.7; of more than SMALL_SEQS, where the
 // other way's plan takes longer, 128 of 512 17.2 and 18.6.  Many workgroups that have little to do cost more than a line of it:
 // 1024 sequences of 32, 46.8 and 38.0.
 constexpr int DIRECT_TOKENS = 1280, DIRECT_UNITS = 2048;
+constexpr int DIRECT_FEW_SEQS = 4, DIRECT_FEW_TOKENS = 1152;  // fp32, 128 dims
 constexpr int64_t DIRECT_SMALL = 1 << 18, DIRECT_LARGE = 1 << 19;  // tokens of all workgroups
 
-bool is_direct(const pq_paged_shared_args &a)
+bool is_direct(const pq_paged_config &cfg, const pq_paged_shared_args &a)
 {
     const int64_t width = (int64_t)a.c.max_blocks << a.c.log_block, units = (int64_t)a.n_seqs * own_tiles(a.G) * a.c.Hkv;
-    return width <= DIRECT_TOKENS && units <= DIRECT_UNITS && units * width <= (a.n_seqs <= SMALL_SEQS ? DIRECT_SMALL : DIRECT_LARGE);
+    const bool few = cfg.dtype == PQ_F32 && cfg.head_dim == 128 && a.n_seqs <= DIRECT_FEW_SEQS;
+    return width <= (few ? DIRECT_FEW_TOKENS : DIRECT_TOKENS) && units <= DIRECT_UNITS && units * width <= (a.n_seqs <= SMALL_SEQS ? DIRECT_SMALL : DIRECT_LARGE);
 }
 
 }  // namespace
@@ -826,7 +830,7 @@ int64_t pq_paged_shared_layout(const pq_paged_ctx *ctx, int n_seqs, int n_groups
 
 hipError_t pq_launch_paged_shared(const pq_paged_ctx *ctx, const pq_paged_shared_args &a, hipStream_t s)
 {
-    if (is_direct(a)) {
+    if (is_direct(ctx->cfg, a)) {
         const dim3 units((unsigned)(a.n_seqs * own_tiles(a.G) * a.c.Hkv));
 #define LAUNCH(T, D) hipLaunchKernelGGL((pq_paged_shared_direct_kernel<T, D>), units, dim3(THREADS), 0, s, a)
         PQ_PAGED_BY_TYPE(ctx->cfg.dtype, ctx->cfg.head_dim, LAUNCH);

@@ -500,3 +500,21 @@ def test_full_precision_of_long_prompts_and_chats(seqs):
     ctx = c.context("f32", 8, 2)
     q, values = queries(rng, c.seqs, 8, 128, "f32")
     check(c.call(ctx, q, empty(c, 8, "f32"), 0.09), *c.expected(values, 0.09), "f32", 128)
+
+
+@pytest.mark.parametrize("dtype,dim,seqs,most", [("f32", 128, 1, 1152), ("f32", 128, 2, 1152), ("f32", 128, 4, 1152), ("f32", 128, 5, 1280),
+                                                 ("f32", 64, 2, 1280), ("f16", 128, 2, 1280), ("bf16", 128, 1, 1280)])
+def test_which_calls_are_short_by_their_tables(dtype, dim, seqs, most):
+    """Up to so many tokens of a table a call takes the way that leaves its workspace alone: what was measured to be faster."""
+    rng = np.random.default_rng(33)
+    c = Groups(rng, [(64, [64 + 300 * (i + 1) // seqs for i in range(seqs)])], 2, dim, 16)
+    for width in (most // 16, most // 16 + 1):
+        ctx = context(dtype, 8, 2, dim, 16, c.n_blocks, width, seqs)
+        table = np.full((seqs, width), -1)
+        n = min(width, c.table.shape[1])
+        table[:, :n] = c.table[:, :n]
+        c.block_table = dev(table)
+        q, values = queries(rng, seqs, 8, dim, dtype)
+        workspace = work(ctx, seqs, 1)
+        check(c.call(ctx, q, empty(c, 8, dtype), 0.1, workspace), *c.expected(values, 0.1), dtype, dim)
+        assert bool((workspace == 255).all()) == (width == most // 16)
