@@ -440,8 +440,10 @@ int pq_paged_copy(pq_paged_ctx *ctx, int32_t n_pairs, const int32_t *src, const 
                   float *to_v_scale, void *hip_stream);
 
 /* pq_paged_decode for groups of requests that begin with the same blocks: those are read once for a group, unless
- * that costs more than it saves.  (What shares little and is short by max_blocks takes one launch, other calls two or three: a
- * call whose requests hold few tokens in wide tables is faster by pq_paged_decode.)
+ * that costs more than it saves.  It takes two or three launches, one where tables are short (max_blocks * block_tokens up to 1280, less for
+ * many requests or wide values): calls of few tokens are faster by pq_paged_decode, whatever they share.  With 32 query and 8 KV heads that is so up to
+ * some 2^15 tokens, those of all requests counted (4 of 1000 tokens 7.4 us there and 9.9 here, 4 of 8192 14.9 and 16.5, of 16384 23.7
+ * and 21.4), but for many requests in short tables (32 of 512 tokens 10.6 us there and 7.4 here).
  *
  *   n_groups     1 .. n_seqs (PQ_ERR_SHAPE, PQ_ERR_CAPACITY otherwise); n_seqs * ceil(Hq / Hkv / 16) * max_blocks *
  *                block_tokens < 2^35 (PQ_ERR_CAPACITY)

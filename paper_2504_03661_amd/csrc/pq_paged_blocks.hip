@@ -10,7 +10,7 @@
 //
 // Fork, free and compact are bound by latency: launches, and loads that need each other (four forks of a prompt of 1000 tokens 3 us, half
 // of 1000 requests with up to 10K tokens ended 9 us in three launches, 2700 blocks compacted 6 us in two).  Copy is bound by HBM:
-// 8192 blocks of 64 KiB for each of K and V 378 us, 5.0 TB/s, 106 % of what a copy of 4 GiB reaches.
+// 7200 blocks of 64 KiB for each of K and V, of a list of 8192 pairs, 378 us, 1.89 GB at 5.0 TB/s, 106 % of what a copy of 4 GiB reaches.
 #include <hip/hip_runtime.h>
 
 #include "pq_paged_scan.h"
@@ -22,7 +22,8 @@ constexpr int ROW_THREADS = 256, LOADS = 4;  // entries of a thread on their way
 // Entries of all block tables together up to which one workgroup does a call, all its threads on all of them: with 4K of them a fork and its
 // copy take 10.3 us, and 13.6 with a grid for the tables; an end, behind a copy of the counts, 10.8 and 15.2; with 7K 11.8 and 13.6,
 // 13.4 and 14.8.  With 8K it is 13.7 and 13.3, 17.2 and 15.1: all atomics go through one compute unit.  (A wavefront a row, 256 requests
-// of 16 blocks: 19.8, 19.4.)
+// of 16 blocks: 19.8, 19.4.)  It is the tables' width that counts, not what the rows hold: four forks of 1000 tokens 10.0 us, and 13.7 with
+// room for 32K tokens a row; six of eight ends 8.2 and 16.0.
 constexpr int ONE_ENTRIES = 7 * SCAN_THREADS;
 
 // what a call's launches hand over, in the context's scratch
@@ -522,8 +523,8 @@ __global__ __launch_bounds__(ROW_THREADS) void pq_paged_renumber_kernel(pq_paged
 constexpr int COPY_THREADS = 256;
 constexpr int COPY_LOADS = 4;  // 16-byte loads of a thread on their way together
 constexpr int COPY_UNIT = COPY_THREADS * COPY_LOADS * 16;
-// Workgroups a compute unit, one after another for the most part: with loads and stores that pass the caches 8192 blocks of 64 KiB
-// (1.9 GB moved) take 382 us with 8 of them, 379 with 32, 377 with 64, and 19 000 pairs of a list of 83 000 206, 199 and 195; those that
+// Workgroups a compute unit, one after another for the most part: with loads and stores that pass the caches 7200 blocks of 64 KiB
+// for each of K and V (1.9 GB moved) take 382 us with 8 of them, 379 with 32, 377 with 64, and 19 000 pairs of a list of 83 000 206, 199 and 195; those that
 // find nothing at the end of a short list cost about a microsecond for each eight.  (Through the caches 388 and 218 us, with 8.)
 constexpr int COPY_PER_CU = 32;
 

@@ -88,7 +88,8 @@ __device__ inline int range_of(const pq_paged_shared_ranges &r, int step)
 
 // The line's `steps` over the workgroups that the groups' jobs leave: those that run beside them get longer ranges, those that take
 // their place when they are done shorter ones, by what the jobs' wavefronts have to do, so that all end together.  Where the ones
-// beside them are done with all of it before others could be with a shortest range, there are only those.
+// beside them are done with all of it before others could be with a shortest range, there are only those.  Where the jobs are as many as
+// the workgroups or more, all ranges are alike: those that have one job fewer than others end earlier.
 __device__ inline pq_paged_shared_ranges cut_line(int steps, float group_keys, int group_jobs, int workgroups)
 {
     pq_paged_shared_ranges r;
