@@ -518,3 +518,27 @@ def test_which_calls_are_short_by_their_tables(dtype, dim, seqs, most):
         workspace = work(ctx, seqs, 1)
         check(c.call(ctx, q, empty(c, 8, dtype), 0.1, workspace), *c.expected(values, 0.1), dtype, dim)
         assert bool((workspace == 255).all()) == (width == most // 16)
+
+
+@pytest.mark.parametrize("seqs", [20, 100, 300])
+def test_a_graph_in_full_precision(seqs):
+    """fp32, 128 dims, recorded before any eager call of its kernels has run in this context; replays with other lengths, eager calls between."""
+    rng = np.random.default_rng(seqs + 1)
+    c = Groups(rng, [(int(s) * 16, [int(s) * 16 + int(n) for n in rng.integers(0, 70, 5)]) for s in rng.integers(0, 30, seqs // 5)], 2, 128, 16)
+    ctx = c.context("f32", 8, 2)
+    workspace, out = work(ctx, c.seqs, seqs // 5), empty(c, 8, "f32")
+    q, values = queries(rng, c.seqs, 8, 128, "f32")
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        c.call(ctx, q, out, 0.1, workspace)
+    for step in range(3):
+        if step:
+            c.lengths = np.minimum(c.lengths, rng.integers(0, 600, c.seqs))
+            c.seq_len.copy_(dev(c.lengths))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check(out, *c.expected(values, 0.1), "f32", 128, f"replay {step}")
+        assert torch.equal(c.call(ctx, q, empty(c, 8, "f32"), 0.1), out)          # eager, a workspace of its own
+    assert pq.pq_paged_device_error(ctx.handle) == 0
